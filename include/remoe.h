@@ -423,6 +423,99 @@ remoe_status remoe_gate_grad(const float *dlogits, const void *x, int32_t x_dtyp
                              int32_t n_experts, int32_t hidden, float *dw,
                              void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * The vocabulary end of a model whose layers are the ones above: what it answers with, and the terms over the
+ * vocabulary that stand beside the router's regularisers in the training objective (Eq. 3: L = L_CE + ...).
+ * With z = logits[t, :], V the vocabulary, tau the temperature:
+ *
+ *   m = max_v z_v,  d_v = (z_v - m) / tau,  S = sum_v exp(d_v) = 1 + rest,  ln p_v = d_v - ln S
+ *
+ *   rest is the sum without the (first) largest logit's own 1: log1p(rest) keeps what ln S loses when one
+ *   token has nearly all of the probability.
+ *
+ * Common to the four calls:
+ *   logits   rows of vocab consecutive values of desc->dtype, `ld` >= vocab values from one row to the next
+ *            (values between vocab and ld are neither read nor written); any alignment of a value
+ *   Arithmetic is fp32 from the logits on (fp64 for the few values per row where differences cancel); sums have a
+ *   fixed order, results repeat bit for bit.  -inf masks a token: probability 0, gradient 0.  A row of nothing but
+ *   -inf has stats (-inf, -1), ln p = -inf for every token, entropy 0 and gradient 0.  A row that holds NaN or +inf
+ *   has rest = NaN (its max is unspecified), and its log probabilities, entropy, losses and gradients are NaN.
+ *   vocab 1..2^24, temperature positive, finite and not below 2^-20; n_tokens 0..2^22 (0 launches nothing).
+ */
+typedef struct {
+    int32_t vocab;         /* V                                                                      */
+    int32_t dtype;         /* remoe_dtype of logits and dlogits                                      */
+    float temperature;     /* tau                                                                    */
+} remoe_head_desc;
+
+/* Bytes of workspace remoe_token_logprobs (with top_n alternatives) and remoe_distill_forward (top_n 0) need; never 0
+ * for valid arguments, 0 with remoe_last_error set otherwise; never less for more tokens.  Host call, no GPU work. */
+size_t remoe_head_workspace_bytes(const remoe_head_desc *desc, int64_t n_tokens, int32_t top_n);
+
+/*
+ * remoe_token_logprobs -- log probabilities of given tokens, entropy and the most probable alternatives:
+ *
+ *   targets         [T] int32 token ids, or NULL;  out_logprob [T] fp32: ln p_target, 0 where the target lies outside
+ *                   0..V-1 (a position to be ignored).  NULL together with targets
+ *   out_entropy     [T] fp32: -sum_v p_v ln p_v, never negative; or NULL
+ *   out_top_idx     [T, top_n] int32: the ids of the top_n largest logits, descending, ties to the lower id (NaN ranks
+ *                   above +inf);  out_top_logprob [T, top_n] fp32: their ln p.  Both NULL when top_n is 0
+ *   out_stats       [T, 2] fp32: (m, rest), what the backward call needs; or NULL
+ *   top_n           0..min(64, vocab);  at least one output is asked for
+ *   workspace       remoe_head_workspace_bytes(desc, T, top_n) bytes, 256-byte aligned; scratch
+ */
+remoe_status remoe_token_logprobs(const remoe_head_desc *desc, const void *logits, int64_t n_tokens, int64_t ld,
+                                  const int32_t *targets, int32_t top_n, float *out_logprob, float *out_entropy,
+                                  int32_t *out_top_idx, float *out_top_logprob, float *out_stats,
+                                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * remoe_token_logprobs_backward -- gradient of sum_t d_logprob[t] logprob[t] + d_entropy[t] entropy[t]:
+ *
+ *   dlogits[t, v] = (1/tau) ( d_logprob[t] (1[v = target] - p_v) - d_entropy[t] p_v (ln p_v + entropy[t]) )
+ *
+ * (cross-entropy of T tokens: d_logprob = -1/T).  The first term is left out where the target lies outside 0..V-1.
+ *   stats           [T, 2] as remoe_token_logprobs wrote them for the same logits and temperature
+ *   d_logprob       [T] fp32, or NULL together with targets;  entropy, d_entropy [T] fp32, or both NULL; one pair is given
+ *   accumulate      0: dlogits is written; 1: added to (in fp32, rounded once)
+ *   dlogits         [T, V] of desc->dtype with row stride ld_d >= vocab.  With accumulate 0 it may be `logits` itself
+ *                   (same pointer and row stride); any other overlap of the two is refused
+ */
+remoe_status remoe_token_logprobs_backward(const remoe_head_desc *desc, const void *logits, int64_t n_tokens, int64_t ld,
+                                           const float *stats, const int32_t *targets, const float *d_logprob,
+                                           const float *entropy, const float *d_entropy, int32_t accumulate,
+                                           void *dlogits, int64_t ld_d, void *stream);
+
+/*
+ * remoe_distill_forward -- divergence of the model from a teacher of which only the K largest logits of every row are kept:
+ *
+ *   loss[t] = sum_j q_j (ln q_j - ln p_id(j)),   terms with q_j = 0 are 0
+ *   q = softmax(teacher_logits[t] / tau) over the row's list            when teacher_lse is NULL
+ *   q_j = exp(teacher_logits[t, j] / tau - teacher_lse[t])              otherwise: the list's share of the teacher's
+ *         distribution, teacher_lse = ln sum_v exp(teacher_v / tau) over its whole vocabulary
+ *
+ *   teacher_idx     [T, K] int32; entries outside 0..V-1 are absent (a shorter list); an id that stands there twice counts
+ *                   as two entries.  teacher_logits [T, K] of teacher_dtype.  teacher_lse [T] fp32 or NULL.  K = top_k 1..256
+ *   out_loss        [T] fp32 (without the factor tau^2 some recipes use);  out_stats [T, 2] fp32 as above, or NULL
+ *   workspace       remoe_head_workspace_bytes(desc, T, 0) bytes, 256-byte aligned; scratch
+ */
+remoe_status remoe_distill_forward(const remoe_head_desc *desc, const void *logits, int64_t n_tokens, int64_t ld,
+                                   const int32_t *teacher_idx, const void *teacher_logits, int32_t teacher_dtype,
+                                   const float *teacher_lse, int32_t top_k, float *out_loss, float *out_stats,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * remoe_distill_backward -- gradient of sum_t d_loss[t] loss[t]:
+ *
+ *   dlogits[t, v] = (d_loss[t] / tau) ( p_v sum_j q_j - sum_{j: id_j = v} q_j )
+ *
+ *   stats, accumulate, dlogits, ld_d   as for remoe_token_logprobs_backward;  d_loss [T] fp32
+ */
+remoe_status remoe_distill_backward(const remoe_head_desc *desc, const void *logits, int64_t n_tokens, int64_t ld,
+                                    const float *stats, const int32_t *teacher_idx, const void *teacher_logits,
+                                    int32_t teacher_dtype, const float *teacher_lse, int32_t top_k, const float *d_loss,
+                                    int32_t accumulate, void *dlogits, int64_t ld_d, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -59,6 +59,15 @@ def lib() -> ctypes.CDLL:
         _lib.oracle_remoe_loss_grad.restype = _c_int
         _lib.oracle_remoe_loss_grad.argtypes = [_c_ptr, _c_ptr, _c_ptr, _c_i64, _c_i64, _c_int, _c_int, _c_ptr, _c_int,
                                                 _c_int, _c_ptr, _c_ptr]
+        _c_dbl = ctypes.c_double
+        _lib.oracle_token_logprobs.restype = _c_int
+        _lib.oracle_token_logprobs.argtypes = [_c_ptr, _c_i64, _c_i64, _c_dbl, _c_ptr, _c_int, _c_ptr, _c_ptr, _c_ptr, _c_ptr, _c_ptr]
+        _lib.oracle_token_logprobs_grad.restype = _c_int
+        _lib.oracle_token_logprobs_grad.argtypes = [_c_ptr, _c_i64, _c_i64, _c_dbl, _c_ptr, _c_ptr, _c_ptr, _c_ptr]
+        _lib.oracle_distill.restype = _c_int
+        _lib.oracle_distill.argtypes = [_c_ptr, _c_i64, _c_i64, _c_dbl, _c_ptr, _c_ptr, _c_ptr, _c_int, _c_ptr, _c_ptr]
+        _lib.oracle_distill_grad.restype = _c_int
+        _lib.oracle_distill_grad.argtypes = [_c_ptr, _c_i64, _c_i64, _c_dbl, _c_ptr, _c_ptr, _c_ptr, _c_int, _c_ptr, _c_ptr]
         _lib.oracle_gate_grad.restype = _c_int
         _lib.oracle_gate_grad.argtypes = [_c_ptr, _c_ptr, _c_i64, _c_int, _c_int, _c_ptr, _c_i64, _c_ptr]
     return _lib
@@ -308,4 +317,62 @@ def gate_grad(dz: torch.Tensor, x: torch.Tensor, pick: Optional[torch.Tensor] = 
         rc = lib().oracle_gate_grad(_p(dz), _p(x), T, N, H, None, 0, _p(out))
     if rc != 0:
         raise ValueError(f"oracle_gate_grad failed ({rc})")
+    return out
+
+
+def _tau(tau: float) -> float:
+    """The temperature as the library gets it: an fp32 value."""
+    return float(torch.tensor(float(tau), dtype=torch.float32))
+
+
+def token_logprobs(logits: torch.Tensor, tau: float, targets: Optional[torch.Tensor], top_n: int):
+    """Log probabilities over the vocabulary.  logits [T, V] fp32 or bf16; targets int32 [T] or None.  Returns a dict:
+    logprob (if targets), entropy fp64 [T], stats fp64 [T, 2] (max, rest of the sum), top_idx int32 and top_logprob [T, n]."""
+    z, targets = _chk(logits.float()), _chk(targets, torch.int32)
+    T, V = z.shape
+    f = lambda *shape: torch.zeros(*shape, dtype=torch.float64)
+    out = {"logprob": f(T), "entropy": f(T), "stats": f(T, 2), "top_idx": torch.zeros(T, top_n, dtype=torch.int32), "top_logprob": f(T, top_n)}
+    rc = lib().oracle_token_logprobs(_p(z), T, V, _tau(tau), _p(targets), top_n, _p(out["logprob"]), _p(out["entropy"]),
+                                     _p(out["top_idx"]), _p(out["top_logprob"]), _p(out["stats"]))
+    if rc != 0:
+        raise ValueError(f"oracle_token_logprobs failed ({rc})")
+    return out
+
+
+def token_logprobs_grad(logits: torch.Tensor, tau: float, targets: Optional[torch.Tensor], d_logprob: Optional[torch.Tensor],
+                        d_entropy: Optional[torch.Tensor]):
+    """Gradient of sum_t d_logprob[t] logprob[t] + d_entropy[t] entropy[t]: fp64 [T, V]."""
+    z, targets = _chk(logits.float()), _chk(targets, torch.int32)
+    d_logprob, d_entropy = _chk(d_logprob, torch.float32), _chk(d_entropy, torch.float32)
+    T, V = z.shape
+    out = torch.zeros(T, V, dtype=torch.float64)
+    rc = lib().oracle_token_logprobs_grad(_p(z), T, V, _tau(tau), _p(targets), _p(d_logprob), _p(d_entropy), _p(out))
+    if rc != 0:
+        raise ValueError(f"oracle_token_logprobs_grad failed ({rc})")
+    return out
+
+
+def distill(logits: torch.Tensor, tau: float, idx: torch.Tensor, teacher_logits: torch.Tensor, lse: Optional[torch.Tensor] = None):
+    """Divergence from a teacher's listed tokens: (loss fp64 [T], stats fp64 [T, 2]).  idx int32, teacher_logits [T, K]; lse fp32 [T]."""
+    z, tl = _chk(logits.float()), _chk(teacher_logits.float())
+    idx, lse = _chk(idx, torch.int32), _chk(lse, torch.float32)
+    T, V = z.shape
+    loss, stats = torch.zeros(T, dtype=torch.float64), torch.zeros(T, 2, dtype=torch.float64)
+    rc = lib().oracle_distill(_p(z), T, V, _tau(tau), _p(idx), _p(tl), _p(lse), idx.shape[1], _p(loss), _p(stats))
+    if rc != 0:
+        raise ValueError(f"oracle_distill failed ({rc})")
+    return loss, stats
+
+
+def distill_grad(logits: torch.Tensor, tau: float, idx: torch.Tensor, teacher_logits: torch.Tensor, d_loss: torch.Tensor,
+                 lse: Optional[torch.Tensor] = None):
+    """Gradient of sum_t d_loss[t] loss[t]: fp64 [T, V]."""
+    z, tl = _chk(logits.float()), _chk(teacher_logits.float())
+    idx, lse = _chk(idx, torch.int32), _chk(lse, torch.float32)
+    T, V = z.shape
+    d_loss = _chk(d_loss, torch.float32)
+    out = torch.zeros(T, V, dtype=torch.float64)
+    rc = lib().oracle_distill_grad(_p(z), T, V, _tau(tau), _p(idx), _p(tl), _p(lse), idx.shape[1], _p(d_loss), _p(out))
+    if rc != 0:
+        raise ValueError(f"oracle_distill_grad failed ({rc})")
     return out

@@ -5,7 +5,7 @@ import subprocess
 import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-SRCS = [os.path.join(HERE, n) for n in ("remoe_oracle.c", "remoe_oracle_cache.c", "remoe_oracle_loss.c")]
+SRCS = [os.path.join(HERE, n) for n in ("remoe_oracle.c", "remoe_oracle_cache.c", "remoe_oracle_loss.c", "remoe_oracle_head.c")]
 LIB = os.path.join(HERE, "liboracle.so")
 
 

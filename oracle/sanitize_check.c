@@ -33,6 +33,10 @@ int oracle_remoe_losses(const float *, const float *, const int32_t *, int64_t, 
 int oracle_remoe_loss_grad(const float *, const float *, const int32_t *, int64_t, int64_t, int, int, const int32_t *, int,
                            int, const double *, double *);
 int oracle_gate_grad(const float *, const float *, int64_t, int, int, const int32_t *, int64_t, double *);
+int oracle_token_logprobs(const float *, int64_t, int64_t, double, const int32_t *, int, double *, double *, int32_t *, double *, double *);
+int oracle_token_logprobs_grad(const float *, int64_t, int64_t, double, const int32_t *, const float *, const float *, double *);
+int oracle_distill(const float *, int64_t, int64_t, double, const int32_t *, const float *, const float *, int, double *, double *);
+int oracle_distill_grad(const float *, int64_t, int64_t, double, const int32_t *, const float *, const float *, int, const float *, double *);
 
 static uint64_t rng_state = 0x9E3779B97F4A7C15ull;
 static uint32_t rnd(void)
@@ -180,6 +184,30 @@ static void loss_case(int64_t S, int64_t T, int N, int K, int window)
     free(dzf); free(x); free(dw); free(dw2);
 }
 
+/* targets and listed ids inside and outside the vocabulary, a row of -inf, a row with NaN */
+static void head_case(int64_t T, int64_t V, int n, int K)
+{
+    float *z = frand((size_t)(T * V)), *tl = frand((size_t)(T * K)), *lse = frand((size_t)T), *up = frand((size_t)T);
+    int32_t *tgt = blk((size_t)T * 4), *idx = blk((size_t)(T * K) * 4), *top = blk((size_t)(T * n) * 4);
+    for (int64_t t = 0; t < T; ++t) tgt[t] = (int32_t)((int64_t)(rnd() % (uint32_t)(V + 2)) - 1);
+    for (int64_t i = 0; i < T * K; ++i) idx[i] = (int32_t)((int64_t)(rnd() % (uint32_t)(V + 2)) - 1);
+    for (int64_t v = 0; v < V; ++v) z[v] = -INFINITY;
+    if (T > 1) z[V] = NAN;
+    tl[0] = -INFINITY;
+    double *lp = blk((size_t)T * 8), *h = blk((size_t)T * 8), *st = blk((size_t)T * 16), *tlp = blk((size_t)(T * n) * 8);
+    double *loss = blk((size_t)T * 8), *dz = blk((size_t)(T * V) * 8);
+    EXPECT(oracle_token_logprobs(z, T, V, 0.7, tgt, n, lp, h, top, tlp, st), 0);
+    EXPECT(oracle_token_logprobs(z, T, V, 0.7, NULL, 0, NULL, NULL, NULL, NULL, st), 0);
+    EXPECT(oracle_token_logprobs(z, T, V, 0.0, tgt, n, lp, h, top, tlp, st), -1);
+    EXPECT(oracle_token_logprobs_grad(z, T, V, 1.0, tgt, up, lse, dz), 0);
+    EXPECT(oracle_token_logprobs_grad(z, T, V, 1.0, NULL, NULL, lse, dz), 0);
+    EXPECT(oracle_distill(z, T, V, 2.0, idx, tl, lse, K, loss, st), 0);
+    EXPECT(oracle_distill(z, T, V, 2.0, idx, tl, NULL, K, loss, NULL), 0);
+    EXPECT(oracle_distill_grad(z, T, V, 2.0, idx, tl, NULL, K, up, dz), 0);
+    EXPECT(oracle_distill_grad(z, T, V, 2.0, idx, tl, lse, K, up, dz), 0);
+    free(z); free(tl); free(lse); free(up); free(tgt); free(idx); free(top); free(lp); free(h); free(st); free(tlp); free(loss); free(dz);
+}
+
 int main(void)
 {
     layer_case(0, 7, 48, 5, 20, 2, 0, 0, 0);        /* fp32, odd sizes */
@@ -196,6 +224,9 @@ int main(void)
     loss_case(2, 12, 8, 2, 4);
     loss_case(1, 1, 4, 1, 3);                       /* one step: no partner, no full window */
     loss_case(1, 40, 16, 4, 7);                     /* lags up to 16, ragged last window */
+    head_case(4, 37, 5, 6);
+    head_case(1, 1, 1, 3);                          /* one token in the vocabulary */
+    head_case(3, 9, 9, 20);                         /* every token an alternative, a list longer than the vocabulary */
     if (fails) { fprintf(stderr, "sanitize_check: %d unexpected result(s)\n", fails); return 1; }
     printf("sanitize_check ok\n");
     return 0;

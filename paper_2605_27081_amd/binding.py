@@ -38,6 +38,15 @@ class LayerDesc(ctypes.Structure):
         return torch.float32 if self.dtype == REMOE_F32 else torch.bfloat16
 
 
+class HeadDesc(ctypes.Structure):
+    """Mirror of remoe_head_desc."""
+    _fields_ = [("vocab", ctypes.c_int32), ("dtype", ctypes.c_int32), ("temperature", ctypes.c_float)]
+
+    @property
+    def torch_dtype(self):
+        return torch.float32 if self.dtype == REMOE_F32 else torch.bfloat16
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -106,6 +115,17 @@ def load_library() -> ctypes.CDLL:
     lib.remoe_gate_grad_workspace_bytes.argtypes = [I64, I32, I32]
     lib.remoe_gate_grad.restype = ctypes.c_int
     lib.remoe_gate_grad.argtypes = [P, P, I32, I64, I32, I32, P, P, SZ, P]
+    HD = ctypes.POINTER(HeadDesc)
+    lib.remoe_head_workspace_bytes.restype = SZ
+    lib.remoe_head_workspace_bytes.argtypes = [HD, I64, I32]
+    lib.remoe_token_logprobs.restype = ctypes.c_int
+    lib.remoe_token_logprobs.argtypes = [HD, P, I64, I64, P, I32, P, P, P, P, P, P, SZ, P]
+    lib.remoe_token_logprobs_backward.restype = ctypes.c_int
+    lib.remoe_token_logprobs_backward.argtypes = [HD, P, I64, I64, P, P, P, P, P, I32, P, I64, P]
+    lib.remoe_distill_forward.restype = ctypes.c_int
+    lib.remoe_distill_forward.argtypes = [HD, P, I64, I64, P, P, I32, P, I32, P, P, P, SZ, P]
+    lib.remoe_distill_backward.restype = ctypes.c_int
+    lib.remoe_distill_backward.argtypes = [HD, P, I64, I64, P, P, P, I32, P, I32, P, I32, P, I64, P]
     _lib = lib
     return lib
 
@@ -325,3 +345,113 @@ def remoe_gate_grad(dlogits: torch.Tensor, x: torch.Tensor, dw: torch.Tensor, wo
     code = REMOE_BF16 if x.dtype == torch.bfloat16 else REMOE_F32
     _check(load_library().remoe_gate_grad(_ptr(dlogits), _ptr(x), code, n_tokens, n_experts, hidden, _ptr(dw),
                                           _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
+
+
+def _dense(t: Optional[torch.Tensor], what: str, shape, dtype: torch.dtype):
+    """Pointer of a contiguous tensor of this shape and type on the current device (NULL for None)."""
+    if t is None:
+        return None
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+        raise RemoeError(f"{what} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+    p = _ptr(t)
+    if t.device.index != torch.cuda.current_device():
+        raise RemoeError(f"{what} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return p
+
+
+def _rows(t: torch.Tensor, what: str, desc: HeadDesc):
+    """Pointer and row stride of a [T, vocab] matrix of the descriptor's type whose rows are dense."""
+    if not t.is_cuda:
+        raise RemoeError("the library takes device tensors")
+    if t.dim() != 2 or t.shape[1] != desc.vocab or t.dtype != desc.torch_dtype:
+        raise RemoeError(f"{what} must be {desc.torch_dtype} [T, {desc.vocab}], got {t.dtype} {list(t.shape)}")
+    if t.device.index != torch.cuda.current_device():
+        raise RemoeError(f"{what} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise RemoeError(f"the values of a row of {what} must follow each other")
+    return t.data_ptr(), max(t.stride(0), desc.vocab) if t.shape[0] < 2 else t.stride(0)
+
+
+def _scratch(t: torch.Tensor):
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise RemoeError("the workspace must be on the current device")
+    return _ptr(t), t.numel() * t.element_size()
+
+
+def remoe_head_workspace_bytes(desc: HeadDesc, n_tokens: int, top_n: int = 0) -> int:
+    n = int(load_library().remoe_head_workspace_bytes(ctypes.byref(desc), n_tokens, top_n))
+    if n == 0:
+        raise RemoeError(f"remoe_head_workspace_bytes: {remoe_last_error()}")
+    return n
+
+
+def remoe_token_logprobs(desc: HeadDesc, logits: torch.Tensor, targets: Optional[torch.Tensor], out_logprob: Optional[torch.Tensor],
+                         out_entropy: Optional[torch.Tensor], out_top_idx: Optional[torch.Tensor],
+                         out_top_logprob: Optional[torch.Tensor], out_stats: Optional[torch.Tensor], workspace: torch.Tensor) -> None:
+    """logits [T, V] with dense rows; targets int32 [T]; out_logprob, out_entropy fp32 [T]; out_top_idx int32 [T, n] and
+    out_top_logprob fp32 [T, n]; out_stats fp32 [T, 2] (max, rest of the sum).  Outputs may be None."""
+    T = logits.shape[0]
+    top_n = 0 if out_top_idx is None else out_top_idx.shape[-1]
+    z, ld = _rows(logits, "logits", desc)
+    ws, ws_bytes = _scratch(workspace)
+    _check(load_library().remoe_token_logprobs(
+        ctypes.byref(desc), z, T, ld, _dense(targets, "targets", (T,), torch.int32), top_n,
+        _dense(out_logprob, "out_logprob", (T,), torch.float32), _dense(out_entropy, "out_entropy", (T,), torch.float32),
+        _dense(out_top_idx, "out_top_idx", (T, top_n), torch.int32),
+        _dense(out_top_logprob, "out_top_logprob", (T, top_n), torch.float32),
+        _dense(out_stats, "out_stats", (T, 2), torch.float32), ws, ws_bytes, _stream()))
+
+
+def remoe_token_logprobs_backward(desc: HeadDesc, logits: torch.Tensor, stats: torch.Tensor, targets: Optional[torch.Tensor],
+                                  d_logprob: Optional[torch.Tensor], entropy: Optional[torch.Tensor], d_entropy: Optional[torch.Tensor],
+                                  dlogits: torch.Tensor, accumulate: bool = False) -> None:
+    """stats fp32 [T, 2] and entropy fp32 [T] from remoe_token_logprobs; d_logprob, d_entropy fp32 [T]; dlogits [T, V] (written,
+    or added to when accumulate; may be logits itself when not)."""
+    T = logits.shape[0]
+    z, ld = _rows(logits, "logits", desc)
+    dz, ld_d = _rows(dlogits, "dlogits", desc)
+    if dlogits.shape[0] != T:
+        raise RemoeError(f"dlogits has {dlogits.shape[0]} rows, logits {T}")
+    _check(load_library().remoe_token_logprobs_backward(
+        ctypes.byref(desc), z, T, ld, _dense(stats, "stats", (T, 2), torch.float32), _dense(targets, "targets", (T,), torch.int32),
+        _dense(d_logprob, "d_logprob", (T,), torch.float32), _dense(entropy, "entropy", (T,), torch.float32),
+        _dense(d_entropy, "d_entropy", (T,), torch.float32), int(bool(accumulate)), dz, ld_d, _stream()))
+
+
+def _teacher(T: int, teacher_idx: torch.Tensor, teacher_logits: torch.Tensor, teacher_lse: Optional[torch.Tensor]):
+    if teacher_idx.dim() != 2:
+        raise RemoeError(f"teacher_idx must be [T, K], got {list(teacher_idx.shape)}")
+    K = teacher_idx.shape[1]
+    if teacher_logits.dtype not in (torch.float32, torch.bfloat16):
+        raise RemoeError(f"teacher_logits must be float32 or bfloat16, got {teacher_logits.dtype}")
+    code = REMOE_BF16 if teacher_logits.dtype == torch.bfloat16 else REMOE_F32
+    return (_dense(teacher_idx, "teacher_idx", (T, K), torch.int32), _dense(teacher_logits, "teacher_logits", (T, K), teacher_logits.dtype),
+            code, _dense(teacher_lse, "teacher_lse", (T,), torch.float32), K)
+
+
+def remoe_distill_forward(desc: HeadDesc, logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logits: torch.Tensor,
+                          teacher_lse: Optional[torch.Tensor], out_loss: torch.Tensor, out_stats: Optional[torch.Tensor],
+                          workspace: torch.Tensor) -> None:
+    """teacher_idx int32 [T, K], teacher_logits fp32 or bf16 [T, K], teacher_lse fp32 [T] or None; out_loss fp32 [T]; out_stats
+    fp32 [T, 2] or None."""
+    T = logits.shape[0]
+    z, ld = _rows(logits, "logits", desc)
+    ws, ws_bytes = _scratch(workspace)
+    _check(load_library().remoe_distill_forward(
+        ctypes.byref(desc), z, T, ld, *_teacher(T, teacher_idx, teacher_logits, teacher_lse),
+        _dense(out_loss, "out_loss", (T,), torch.float32), _dense(out_stats, "out_stats", (T, 2), torch.float32), ws, ws_bytes, _stream()))
+
+
+def remoe_distill_backward(desc: HeadDesc, logits: torch.Tensor, stats: torch.Tensor, teacher_idx: torch.Tensor,
+                           teacher_logits: torch.Tensor, teacher_lse: Optional[torch.Tensor], d_loss: torch.Tensor,
+                           dlogits: torch.Tensor, accumulate: bool = False) -> None:
+    """stats fp32 [T, 2] from remoe_distill_forward; d_loss fp32 [T]; dlogits as for remoe_token_logprobs_backward."""
+    T = logits.shape[0]
+    z, ld = _rows(logits, "logits", desc)
+    dz, ld_d = _rows(dlogits, "dlogits", desc)
+    if dlogits.shape[0] != T:
+        raise RemoeError(f"dlogits has {dlogits.shape[0]} rows, logits {T}")
+    _check(load_library().remoe_distill_backward(
+        ctypes.byref(desc), z, T, ld, _dense(stats, "stats", (T, 2), torch.float32),
+        *_teacher(T, teacher_idx, teacher_logits, teacher_lse), _dense(d_loss, "d_loss", (T,), torch.float32), int(bool(accumulate)),
+        dz, ld_d, _stream()))

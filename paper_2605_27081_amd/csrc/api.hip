@@ -711,5 +711,166 @@ remoe_status remoe_gate_grad(const float *dlogits, const void *x, int32_t x_dtyp
     return launch_gate_grad(dlogits, x, x_dtype, n_tokens, n_experts, hidden, dw, workspace, static_cast<hipStream_t>(stream));
 }
 
+constexpr int MAX_VOCAB = 1 << 24;
+constexpr int MAX_TOP_N = 64;
+constexpr int MAX_TEACHER_K = 256;
+
+static remoe_status validate_head(const remoe_head_desc *d, int64_t T)
+{
+    if (!d) return fail(REMOE_E_INVALID_ARG, "desc is NULL");
+    if (d->vocab < 1 || d->vocab > MAX_VOCAB) return fail(REMOE_E_INVALID_ARG, "vocab %d outside 1..%d", d->vocab, MAX_VOCAB);
+    if (d->dtype != REMOE_F32 && d->dtype != REMOE_BF16)
+        return fail(REMOE_E_INVALID_ARG, "dtype %d is neither REMOE_F32 nor REMOE_BF16", d->dtype);
+    if (!(d->temperature >= 0x1p-20f) || d->temperature > 3.0e38f)
+        return fail(REMOE_E_INVALID_ARG, "temperature must be finite and at least 2^-20");
+    if (T < 0 || T > MAX_TOKENS) return fail(REMOE_E_INVALID_ARG, "n_tokens %lld outside 0..%lld", (long long)T, (long long)MAX_TOKENS);
+    return REMOE_OK;
+}
+
+static remoe_status validate_rows(const remoe_head_desc *d, const void *rows, int64_t ld, const char *what)
+{
+    if (!rows) return fail(REMOE_E_INVALID_ARG, "%s is NULL", what);
+    if (ld < d->vocab || ld > (int64_t)1 << 32)
+        return fail(REMOE_E_INVALID_ARG, "row stride %lld of %s outside vocab..2^32", (long long)ld, what);
+    if ((uintptr_t)rows & (d->dtype == REMOE_F32 ? 3 : 1)) return fail(REMOE_E_INVALID_ARG, "%s is not aligned to its values", what);
+    return REMOE_OK;
+}
+
+static remoe_status validate_head_workspace(const remoe_head_desc *d, int64_t T, int32_t top_n, const void *workspace, size_t bytes)
+{
+    const size_t need = head_workspace_bytes(d->dtype, d->vocab, T, top_n);
+    if (!workspace || ((uintptr_t)workspace & 255)) return fail(REMOE_E_WORKSPACE, "workspace is NULL or not 256-byte aligned");
+    if (bytes < need) return fail(REMOE_E_WORKSPACE, "workspace has %zu bytes, %zu needed", bytes, need);
+    return REMOE_OK;
+}
+
+static remoe_status validate_teacher(const int32_t *idx, const void *logits, int32_t dtype, const float *lse, int32_t top_k)
+{
+    if (top_k < 1 || top_k > MAX_TEACHER_K) return fail(REMOE_E_INVALID_ARG, "top_k %d outside 1..%d", top_k, MAX_TEACHER_K);
+    if (dtype != REMOE_F32 && dtype != REMOE_BF16)
+        return fail(REMOE_E_INVALID_ARG, "teacher_dtype %d is neither REMOE_F32 nor REMOE_BF16", dtype);
+    if (!idx || !logits) return fail(REMOE_E_INVALID_ARG, "teacher_idx and teacher_logits must not be NULL");
+    if (((uintptr_t)idx & 3) || ((uintptr_t)lse & 3) || ((uintptr_t)logits & (dtype == REMOE_F32 ? 3 : 1)))
+        return fail(REMOE_E_INVALID_ARG, "a teacher's tensor is not aligned to its values");
+    return REMOE_OK;
+}
+
+static remoe_status validate_gradient(const remoe_head_desc *d, const void *logits, int64_t T, int64_t ld, const float *stats,
+                                      int32_t accumulate, const void *dlogits, int64_t ld_d)
+{
+    remoe_status st = validate_rows(d, logits, ld, "logits");
+    if (st == REMOE_OK) st = validate_rows(d, dlogits, ld_d, "dlogits");
+    if (st != REMOE_OK) return st;
+    if (!stats || ((uintptr_t)stats & 3)) return fail(REMOE_E_INVALID_ARG, "stats is NULL or not aligned to its values");
+    if (accumulate != 0 && accumulate != 1) return fail(REMOE_E_INVALID_ARG, "accumulate must be 0 or 1");
+    const uintptr_t es = d->dtype == REMOE_F32 ? 4 : 2, z = (uintptr_t)logits, g = (uintptr_t)dlogits;
+    if (z == g && (ld == ld_d || T == 1)) {
+        if (accumulate) return fail(REMOE_E_INVALID_ARG, "dlogits must not be logits when accumulate is set");
+        return REMOE_OK;
+    }
+    const uintptr_t z_end = z + es * (uintptr_t)((T - 1) * ld + d->vocab), g_end = g + es * (uintptr_t)((T - 1) * ld_d + d->vocab);
+    if (z < g_end && g < z_end) return fail(REMOE_E_INVALID_ARG, "dlogits overlaps logits without being the same rows");
+    return REMOE_OK;
+}
+
+size_t remoe_head_workspace_bytes(const remoe_head_desc *desc, int64_t n_tokens, int32_t top_n)
+{
+    if (validate_head(desc, n_tokens) != REMOE_OK) return 0;
+    if (top_n < 0 || top_n > MAX_TOP_N || top_n > desc->vocab) {
+        set_error("top_n %d outside 0..min(%d, vocab)", top_n, MAX_TOP_N);
+        return 0;
+    }
+    return head_workspace_bytes(desc->dtype, desc->vocab, n_tokens, top_n);
+}
+
+remoe_status remoe_token_logprobs(const remoe_head_desc *desc, const void *logits, int64_t n_tokens, int64_t ld, const int32_t *targets,
+                                  int32_t top_n, float *out_logprob, float *out_entropy, int32_t *out_top_idx, float *out_top_logprob,
+                                  float *out_stats, void *workspace, size_t workspace_bytes, void *stream)
+{
+    remoe_status st = validate_head(desc, n_tokens);
+    if (st != REMOE_OK) return st;
+    if (top_n < 0 || top_n > MAX_TOP_N || top_n > desc->vocab)
+        return fail(REMOE_E_INVALID_ARG, "top_n %d outside 0..min(%d, vocab)", top_n, MAX_TOP_N);
+    if (n_tokens == 0) return REMOE_OK;
+    if (!targets != !out_logprob) return fail(REMOE_E_INVALID_ARG, "targets and out_logprob go together");
+    if ((top_n > 0) != (out_top_idx != nullptr) || (top_n > 0) != (out_top_logprob != nullptr))
+        return fail(REMOE_E_INVALID_ARG, "out_top_idx and out_top_logprob go with top_n > 0");
+    if (!out_logprob && !out_entropy && !out_top_idx && !out_stats) return fail(REMOE_E_INVALID_ARG, "no output is asked for (all are NULL)");
+    if (((uintptr_t)targets | (uintptr_t)out_logprob | (uintptr_t)out_entropy | (uintptr_t)out_top_idx | (uintptr_t)out_top_logprob |
+         (uintptr_t)out_stats) & 3)
+        return fail(REMOE_E_INVALID_ARG, "targets or an output is not aligned to its values");
+    st = validate_rows(desc, logits, ld, "logits");
+    if (st == REMOE_OK) st = validate_head_workspace(desc, n_tokens, top_n, workspace, workspace_bytes);
+    if (st != REMOE_OK) return st;
+    HeadArgs a{};
+    a.logits = logits; a.dtype = desc->dtype; a.T = n_tokens; a.ld = ld; a.V = desc->vocab; a.tau = desc->temperature;
+    a.targets = targets; a.top_n = top_n; a.logprob = out_logprob; a.entropy = out_entropy;
+    a.top_idx = out_top_idx; a.top_logprob = out_top_logprob; a.stats = out_stats; a.workspace = workspace;
+    return launch_head_forward(a, static_cast<hipStream_t>(stream));
+}
+
+remoe_status remoe_token_logprobs_backward(const remoe_head_desc *desc, const void *logits, int64_t n_tokens, int64_t ld, const float *stats,
+                                           const int32_t *targets, const float *d_logprob, const float *entropy, const float *d_entropy,
+                                           int32_t accumulate, void *dlogits, int64_t ld_d, void *stream)
+{
+    remoe_status st = validate_head(desc, n_tokens);
+    if (st != REMOE_OK) return st;
+    if (n_tokens == 0) return REMOE_OK;
+    if (!targets != !d_logprob) return fail(REMOE_E_INVALID_ARG, "targets and d_logprob go together");
+    if (!entropy != !d_entropy) return fail(REMOE_E_INVALID_ARG, "entropy and d_entropy go together");
+    if (!d_logprob && !d_entropy) return fail(REMOE_E_INVALID_ARG, "neither d_logprob nor d_entropy is given (both are NULL)");
+    if (((uintptr_t)targets | (uintptr_t)d_logprob | (uintptr_t)entropy | (uintptr_t)d_entropy) & 3)
+        return fail(REMOE_E_INVALID_ARG, "a row's input is not aligned to its values");
+    st = validate_gradient(desc, logits, n_tokens, ld, stats, accumulate, dlogits, ld_d);
+    if (st != REMOE_OK) return st;
+    HeadGradArgs a{};
+    a.logits = logits; a.dlogits = dlogits; a.dtype = desc->dtype; a.T = n_tokens; a.ld = ld; a.ld_d = ld_d; a.V = desc->vocab;
+    a.tau = desc->temperature; a.accumulate = accumulate; a.stats = stats;
+    a.targets = targets; a.d_logprob = d_logprob; a.entropy = entropy; a.d_entropy = d_entropy;
+    return launch_head_backward(a, static_cast<hipStream_t>(stream));
+}
+
+remoe_status remoe_distill_forward(const remoe_head_desc *desc, const void *logits, int64_t n_tokens, int64_t ld, const int32_t *teacher_idx,
+                                   const void *teacher_logits, int32_t teacher_dtype, const float *teacher_lse, int32_t top_k,
+                                   float *out_loss, float *out_stats, void *workspace, size_t workspace_bytes, void *stream)
+{
+    remoe_status st = validate_head(desc, n_tokens);
+    if (st != REMOE_OK) return st;
+    if (n_tokens == 0) return REMOE_OK;
+    st = validate_teacher(teacher_idx, teacher_logits, teacher_dtype, teacher_lse, top_k);
+    if (st != REMOE_OK) return st;
+    if (!out_loss) return fail(REMOE_E_INVALID_ARG, "out_loss is NULL");
+    if (((uintptr_t)out_loss | (uintptr_t)out_stats) & 3) return fail(REMOE_E_INVALID_ARG, "an output is not aligned to its values");
+    st = validate_rows(desc, logits, ld, "logits");
+    if (st == REMOE_OK) st = validate_head_workspace(desc, n_tokens, 0, workspace, workspace_bytes);
+    if (st != REMOE_OK) return st;
+    HeadArgs a{};
+    a.logits = logits; a.dtype = desc->dtype; a.T = n_tokens; a.ld = ld; a.V = desc->vocab; a.tau = desc->temperature;
+    a.teacher_idx = teacher_idx; a.teacher_logits = teacher_logits; a.teacher_dtype = teacher_dtype; a.K = top_k;
+    a.teacher_lse = teacher_lse; a.loss = out_loss; a.stats = out_stats; a.workspace = workspace;
+    return launch_head_forward(a, static_cast<hipStream_t>(stream));
+}
+
+remoe_status remoe_distill_backward(const remoe_head_desc *desc, const void *logits, int64_t n_tokens, int64_t ld, const float *stats,
+                                    const int32_t *teacher_idx, const void *teacher_logits, int32_t teacher_dtype,
+                                    const float *teacher_lse, int32_t top_k, const float *d_loss, int32_t accumulate, void *dlogits,
+                                    int64_t ld_d, void *stream)
+{
+    remoe_status st = validate_head(desc, n_tokens);
+    if (st != REMOE_OK) return st;
+    if (n_tokens == 0) return REMOE_OK;
+    st = validate_teacher(teacher_idx, teacher_logits, teacher_dtype, teacher_lse, top_k);
+    if (st != REMOE_OK) return st;
+    if (!d_loss || ((uintptr_t)d_loss & 3)) return fail(REMOE_E_INVALID_ARG, "d_loss is NULL or not aligned to its values");
+    st = validate_gradient(desc, logits, n_tokens, ld, stats, accumulate, dlogits, ld_d);
+    if (st != REMOE_OK) return st;
+    HeadGradArgs a{};
+    a.logits = logits; a.dlogits = dlogits; a.dtype = desc->dtype; a.T = n_tokens; a.ld = ld; a.ld_d = ld_d; a.V = desc->vocab;
+    a.tau = desc->temperature; a.accumulate = accumulate; a.stats = stats;
+    a.teacher_idx = teacher_idx; a.teacher_logits = teacher_logits; a.teacher_dtype = teacher_dtype; a.K = top_k;
+    a.teacher_lse = teacher_lse; a.d_loss = d_loss;
+    return launch_head_backward(a, static_cast<hipStream_t>(stream));
+}
+
 #pragma GCC visibility pop
 }  // extern "C"

@@ -185,6 +185,51 @@ size_t gate_grad_workspace_bytes(int64_t T, int N, int H);
 remoe_status launch_gate_grad(const float *dz, const void *x, int x_dtype, int64_t T, int N, int H, float *dw, void *workspace,
                               hipStream_t stream);
 
+// Rows of logits over the vocabulary (head.hip, head_grad.hip): log probabilities, entropy, alternatives, distillation.
+struct HeadArgs {
+    const void *logits;
+    int dtype;
+    int64_t T, ld;
+    int V;
+    float tau;
+    // what is asked of a row: log probabilities ...
+    const int32_t *targets;
+    int top_n;
+    float *logprob, *entropy;
+    int32_t *top_idx;
+    float *top_logprob;
+    // ... or the divergence from a teacher's list (teacher_idx not NULL)
+    const int32_t *teacher_idx;
+    const void *teacher_logits;
+    int teacher_dtype, K;
+    const float *teacher_lse;
+    float *loss;
+    float *stats;             // [T, 2] or NULL
+    void *workspace;
+};
+size_t head_workspace_bytes(int dtype, int V, int64_t T, int top_n);
+remoe_status launch_head_forward(const HeadArgs &a, hipStream_t stream);
+
+struct HeadGradArgs {
+    const void *logits;
+    void *dlogits;
+    int dtype;
+    int64_t T, ld, ld_d;
+    int V;
+    float tau;
+    int accumulate;
+    const float *stats;
+    // log probabilities and entropy ...
+    const int32_t *targets;
+    const float *d_logprob, *entropy, *d_entropy;
+    // ... or a teacher's list (teacher_idx not NULL)
+    const int32_t *teacher_idx;
+    const void *teacher_logits;
+    int teacher_dtype, K;
+    const float *teacher_lse, *d_loss;
+};
+remoe_status launch_head_backward(const HeadGradArgs &a, hipStream_t stream);
+
 // Plain copy of known size (yardstick for hardware byte counters).
 remoe_status launch_copy_probe(void *dst, const void *src, size_t bytes, hipStream_t stream);
 

@@ -1,0 +1,535 @@
+"""GPU parity over the vocabulary: log probabilities, entropy, alternatives, distillation and their gradients against the
+fp64 oracle, on every kind of row, length and alignment."""
+import pytest
+import torch
+
+import oracle
+import paper_2605_27081_amd as remoe
+from head_cases import HALF, KINDS, STEP, SUM_TOL, close, grad_tol, log_p_tol, log_probs, rows
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def _tau(tau):
+    return float(torch.tensor(tau, dtype=torch.float32))
+
+
+def _desc(vocab, dtype, tau):
+    return remoe.HeadDesc(vocab, remoe.REMOE_BF16 if dtype == BF16 else remoe.REMOE_F32, tau)
+
+
+def _to_device(z, ld=None, shift=0):
+    """The same rows on the device, `ld` values apart, the first `shift` values into a buffer; everything else is NaN."""
+    T, V = z.shape
+    ld = ld or V
+    buf = torch.full((T * ld + shift + 8,), float("nan"), dtype=z.dtype, device=DEV)
+    view = buf[shift:shift + T * ld].view(T, ld)[:, :V]
+    view.copy_(z)
+    return view
+
+
+def _out(*shape, dtype=F32):
+    return torch.full(shape, -77, dtype=dtype, device=DEV)
+
+
+def _workspace(desc, T, n=0):
+    # of exactly the stated size, with guard bytes behind it
+    size = remoe.remoe_head_workspace_bytes(desc, T, n)
+    buf = torch.full((size + 256,), 0x5A, dtype=torch.uint8, device=DEV)
+    return buf[:size], buf[size:]
+
+
+def _logprobs(z_dev, tau, tgt, n, entropy=True, stats=True):
+    T, V = z_dev.shape
+    desc = _desc(V, z_dev.dtype, tau)
+    out = {"logprob": _out(T) if tgt is not None else None, "entropy": _out(T) if entropy else None,
+           "top_idx": _out(T, n, dtype=torch.int32) if n else None, "top_logprob": _out(T, n) if n else None,
+           "stats": _out(T, 2) if stats else None}
+    ws, guard = _workspace(desc, T, n)
+    remoe.remoe_token_logprobs(desc, z_dev, None if tgt is None else tgt.to(DEV), out["logprob"], out["entropy"], out["top_idx"],
+                               out["top_logprob"], out["stats"], ws)
+    torch.cuda.synchronize()
+    assert (guard == 0x5A).all(), "written behind the workspace"
+    return out
+
+
+def _check_stats(got, want):
+    ok = ~torch.isnan(want[:, 1])
+    assert torch.equal(got.cpu()[ok, 0], want[ok, 0].float()), "row maxima are exact"
+    close(got[:, 1], want[:, 1], SUM_TOL * want[:, 1].abs() + STEP, "rest")
+
+
+def _check_logprobs(got, z, tau, tgt, n):
+    tau = _tau(tau)
+    want = oracle.token_logprobs(z, tau, tgt, n)
+    st = want["stats"]
+    if got["stats"] is not None:
+        _check_stats(got["stats"], st)
+    if tgt is not None:
+        there = (tgt >= 0) & (tgt < z.shape[1])
+        _, d = log_probs(z, tau, st)
+        d = d.gather(1, tgt.long().clamp(0, z.shape[1] - 1)[:, None])[:, 0]
+        d = torch.where(torch.isfinite(d), d, 0.0)
+        tol = torch.where(there, log_p_tol(st, d, want["logprob"].nan_to_num(0, 0, 0)), torch.zeros_like(d))
+        close(got["logprob"], want["logprob"], tol.nan_to_num(0.0), "logprob")
+    if got["entropy"] is not None:
+        # two sums, both positive, and the quotient
+        close(got["entropy"], want["entropy"], (2 * SUM_TOL + 8 * STEP) * want["entropy"].nan_to_num(0.0), "entropy")
+        assert not bool((got["entropy"] < 0).any())
+    if n:
+        assert torch.equal(got["top_idx"].cpu(), want["top_idx"]), "alternatives"
+        _, d = log_probs(z, tau, st)
+        d = d.gather(1, want["top_idx"].long())
+        d = torch.where(torch.isfinite(d), d, 0.0)
+        close(got["top_logprob"], want["top_logprob"], log_p_tol(st, d, want["top_logprob"].nan_to_num(0, 0, 0)).nan_to_num(0.0), "top_logprob")
+
+
+def _targets(seed, z):
+    T, V = z.shape
+    g = torch.Generator().manual_seed(seed)
+    tgt = torch.randint(0, V, (T,), generator=g).int()
+    tgt[::3] = z[::3].float().nan_to_num(-1.0).argmax(1).int()
+    if T > 4:
+        tgt[3], tgt[4] = -100, V
+    return tgt
+
+
+SIZES = [1, 2, 3, 7, 8, 9, 15, 16, 17, 64, 255, 256, 257, 511, 2047, 2048, 4095, 4097, 8191, 8192, 8193, 16384, 20011]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("vocab", SIZES)
+def test_every_kind_of_row(vocab, dtype):
+    for tau, n, shift in ((1.0, min(5, vocab), 0), (0.7, min(64, vocab), 1)):
+        print(f"log probabilities V={vocab} {dtype} tau={tau} n={n} shift={shift}", flush=True)
+        z = rows(vocab, KINDS, vocab, dtype)
+        tgt = _targets(vocab, z)
+        _check_logprobs(_logprobs(_to_device(z, vocab + 3 * shift, shift), tau, tgt, n), z, tau, tgt, n)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shift", [0, 1, 2, 3, 5, 7])
+@pytest.mark.parametrize("ld", [1003, 1004, 1008, 1024])
+def test_strides_and_alignments(dtype, shift, ld):
+    print(f"strides ld={ld} shift={shift} {dtype}", flush=True)
+    z = rows(ld + shift, ("plain", "masked", "ties", "peaked", "ascending"), 1003, dtype)
+    tgt = _targets(shift, z)
+    _check_logprobs(_logprobs(_to_device(z, ld, shift), 1.0, tgt, 7), z, 1.0, tgt, 7)
+
+
+@pytest.mark.parametrize("T", [1, 2, 3, 63, 130, 600, 1400, 3000])
+def test_numbers_of_rows(T):
+    """Few rows are shared by several workgroups, many have one each."""
+    V = 9001
+    print(f"rows T={T} V={V}", flush=True)
+    kinds = [KINDS[i % len(KINDS)] if T < 200 else ("plain", "masked", "ties")[i % 3] for i in range(T)]
+    z = rows(T, kinds, V, BF16)
+    tgt = _targets(T, z)
+    _check_logprobs(_logprobs(_to_device(z), 0.7, tgt, 20), z, 0.7, tgt, 20)
+
+
+@pytest.mark.parametrize("T,V,dtype,n", [(1, 151936, BF16, 20), (2, 300001, BF16, 64), (1, 300001, F32, 1), (3, 100003, F32, 64), (1, 1 << 20, BF16, 64)])
+def test_large_vocabularies(T, V, dtype, n):
+    print(f"large vocabulary T={T} V={V} {dtype} n={n}", flush=True)
+    z = rows(V, [("plain", "few", "ties")[t % 3] for t in range(T)], V, dtype)
+    tgt = _targets(V, z)
+    _check_logprobs(_logprobs(_to_device(z), 1.0, tgt, n), z, 1.0, tgt, n)
+
+
+def test_outputs_that_are_not_asked_for():
+    V = 777
+    z = rows(4, KINDS, V, F32)
+    tgt = _targets(4, z)
+    zd = _to_device(z)
+    full = _logprobs(zd, 1.0, tgt, 9)
+    for kw in (dict(tgt=None, n=0, entropy=False, stats=True), dict(tgt=None, n=9, entropy=False, stats=False),
+               dict(tgt=tgt, n=0, entropy=False, stats=False), dict(tgt=None, n=0, entropy=True, stats=False)):
+        part = _logprobs(zd, 1.0, kw["tgt"], kw["n"], kw["entropy"], kw["stats"])
+        for k, v in part.items():
+            if v is not None:
+                assert torch.equal(v.view(torch.int32), full[k].view(torch.int32)), k
+
+
+def test_clustered_and_periodic_rows():
+    """Alternatives that all lie with a few threads of a workgroup: runs, periods of every power of two, one block."""
+    V, n = 32768, 64
+    base = 0.1 * torch.arange(V, dtype=torch.float32).remainder(97)
+    z = []
+    for period in (1, 8, 32, 256, 1024, 2048, 4096, 8192):
+        row = base.clone()
+        row[::period] += 50.0
+        z.append(row)
+    row = base.clone()
+    row[12345:12345 + 3000] += 50.0 + torch.arange(3000) * 0.01
+    z.append(row)
+    row = base.clone()
+    row[(torch.arange(V) // 8) % 256 == 3] += 40.0 + 0.001 * torch.arange(V)[(torch.arange(V) // 8) % 256 == 3]
+    z.append(row)
+    for dtype in (F32, BF16):
+        for T in (1, 700):
+            zz = torch.stack(z).to(dtype)
+            if T > 1:
+                zz = zz.repeat((T + len(z) - 1) // len(z), 1)[:T].contiguous()
+            print(f"clustered rows {dtype} T={zz.shape[0]}", flush=True)
+            _check_logprobs(_logprobs(_to_device(zz), 1.0, None, n), zz, 1.0, None, n)
+
+
+# ---- gradients ------------------------------------------------------------------------------------
+
+def _gradient_buffers(z, ld, shift, accumulate, seed=5):
+    T, V = z.shape
+    prior = torch.randn(T, V, generator=torch.Generator().manual_seed(seed)).to(z.dtype)
+    buf = torch.full((T * ld + shift + 8,), 3.0, dtype=z.dtype, device=DEV)
+    view = buf[shift:shift + T * ld].view(T, ld)[:, :V]
+    if accumulate:
+        view.copy_(prior)
+    outside = torch.ones_like(buf, dtype=torch.bool)
+    outside[shift:shift + T * ld].view(T, ld)[:, :V] = False
+    return view, buf, outside, prior
+
+
+def _stats_on_device(z_dev, tau):
+    T, V = z_dev.shape
+    out = _logprobs(z_dev, tau, None, 0)
+    return out["stats"], out["entropy"]
+
+
+def _check_gradient(got, want, tol, prior, dtype, what):
+    want = want + (prior.double() if prior is not None else 0.0)
+    close(got, want, tol + (HALF[dtype] + 2 * STEP) * want.abs().nan_to_num(0, 0, 0), what)
+
+
+def _logprob_gradient(z, tau, tgt, dl, dh, ld=None, shift=0, ld_d=None, shift_d=0, accumulate=False, in_place=False):
+    T, V = z.shape
+    zd = _to_device(z, ld, shift)
+    stats, entropy = _stats_on_device(zd, tau)
+    out, buf, outside, prior = _gradient_buffers(z, ld_d or V, shift_d, accumulate)
+    if in_place:
+        out = zd
+    dev = lambda t: None if t is None else t.to(DEV)
+    remoe.remoe_token_logprobs_backward(_desc(V, z.dtype, tau), zd, stats, dev(tgt), dev(dl), entropy if dh is not None else None, dev(dh),
+                                        out, accumulate)
+    torch.cuda.synchronize()
+    assert (buf[outside] == 3.0).all(), "written outside the rows"
+    tau = _tau(tau)
+    st = oracle.token_logprobs(z, tau, None, 0)
+    want = oracle.token_logprobs_grad(z, tau, tgt, dl, dh)
+    one = torch.ones(T) / tau
+    stt = st["stats"]
+    lp, d = log_probs(z, tau, stt)
+    tol = torch.zeros_like(want)
+    if dl is not None:
+        there = ((tgt >= 0) & (tgt < V)).double()
+        g = (dl.double().abs() * there * one)[:, None]
+        tol += grad_tol(z, tau, stt, g)
+        at = tgt.long().clamp(0, V - 1)[:, None]
+        tol.scatter_add_(1, at, g * (SUM_TOL + 4 * STEP) * -torch.expm1(lp.gather(1, at)))
+    if dh is not None:
+        # p's error times (ln p + H), and that sum's own: two roundings of d, the sum's logarithm, the entropy's error
+        h = (dh.double().abs() * one)[:, None]
+        H = st["entropy"][:, None]
+        inner = lp.abs().clamp(max=200.0) + H
+        tol += grad_tol(z, tau, stt, h) * inner + h * torch.exp(lp) * (8 * STEP * inner + 3 * SUM_TOL * (H + 1.0))
+    _check_gradient(out, want, tol.nan_to_num(0.0), prior if accumulate else None, z.dtype, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("vocab", [1, 2, 7, 8, 9, 31, 255, 257, 1003, 4096, 8193, 20011])
+def test_log_probability_gradient(vocab, dtype):
+    z = rows(vocab + 1, KINDS, vocab, dtype)
+    T = len(KINDS)
+    g = torch.Generator().manual_seed(vocab)
+    tgt, dl, dh = _targets(vocab, z), torch.randn(T, generator=g), torch.randn(T, generator=g)
+    for i, kw in enumerate((dict(tgt=tgt, dl=dl, dh=None), dict(tgt=tgt, dl=dl, dh=dh), dict(tgt=None, dl=None, dh=dh, accumulate=True),
+                            dict(tgt=tgt, dl=dl, dh=dh, in_place=True), dict(tgt=tgt, dl=dl, dh=None, accumulate=True))):
+        print(f"gradient V={vocab} {dtype} variant {i}", flush=True)
+        _logprob_gradient(z, (1.0, 0.7, 2.0, 1.0, 1.0)[i], **kw)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("shift,shift_d", [(0, 0), (1, 1), (0, 1), (3, 0), (5, 2), (7, 7)])
+def test_gradient_strides_and_alignments(dtype, shift, shift_d):
+    z = rows(shift, ("plain", "masked", "peaked", "plain", "lowest", "plain"), 1003, dtype)
+    T = z.shape[0]
+    g = torch.Generator().manual_seed(shift)
+    tgt, dl = _targets(1, z), torch.randn(T, generator=g)
+    idx, tl, lse = _teacher(3, z, 9)
+    for ld, ld_d in ((1003, 1003), (1024, 1003), (1004, 1011)):
+        for accumulate in (False, True):
+            print(f"gradient strides {ld} {ld_d} shifts {shift} {shift_d} {dtype} accumulate={accumulate}", flush=True)
+            _logprob_gradient(z, 1.0, tgt, dl, dl, ld, shift, ld_d, shift_d, accumulate)
+            _distill_gradient(z, 1.0, idx, tl, None, dl, ld, shift, ld_d, shift_d, accumulate)
+
+
+# ---- distillation ---------------------------------------------------------------------------------
+
+def _teacher(seed, z, K, dtype=F32):
+    """The teacher's K largest logits of every row near the student's; a shorter list, an id twice, an entry at -inf."""
+    T, V = z.shape
+    g = torch.Generator().manual_seed(seed)
+    full = z.float().nan_to_num(0.0, 3.0, -8.0).clamp(-30, 30) + torch.randn(T, V, generator=g)
+    k = min(K, V)
+    vals, at = torch.topk(full, k, 1)
+    idx = torch.full((T, K), -1, dtype=torch.int32)
+    tl = torch.zeros(T, K)
+    idx[:, :k], tl[:, :k] = at.int(), vals
+    lse = torch.logsumexp(full, 1)
+    if T > 4 and K > 2:
+        idx[1, K // 2:] = -1
+        idx[2, -1] = V
+        idx[3, -1] = idx[3, 0]
+        tl[4, 1] = -torch.inf
+    if T > 5:
+        idx[5] = -1                                        # no list at all
+    return idx, tl.to(dtype), lse
+
+
+def _teacher_entries(z, tau, idx, tl, lse):
+    V = z.shape[1]
+    there = (idx >= 0) & (idx < V) & (tl.float() > -torch.inf)
+    t = torch.where(there, tl.double(), -torch.inf) / tau
+    lq = t - (lse.double()[:, None] if lse is not None else torch.logsumexp(t, 1, keepdim=True))
+    q = torch.where(there, lq.exp(), 0.0)
+    return there, q, torch.where(there, lq, 0.0)
+
+
+def _distill(z_dev, tau, idx, tl, lse):
+    T, V = z_dev.shape
+    desc = _desc(V, z_dev.dtype, tau)
+    loss, stats = _out(T), _out(T, 2)
+    ws, guard = _workspace(desc, T)
+    remoe.remoe_distill_forward(desc, z_dev, idx.to(DEV), tl.to(DEV), None if lse is None else lse.to(DEV), loss, stats, ws)
+    torch.cuda.synchronize()
+    assert (guard == 0x5A).all(), "written behind the workspace"
+    return loss, stats
+
+
+def _check_distill(z, tau, K, use_lse, tdtype=F32, ld=None, shift=0):
+    T, V = z.shape
+    idx, tl, lse = _teacher(V + K, z, K, tdtype)
+    lse = lse if use_lse else None
+    loss, stats = _distill(_to_device(z, ld, shift), tau, idx, tl, lse)
+    tau = _tau(tau)
+    want, st = oracle.distill(z, tau, idx, tl, lse)
+    _check_stats(stats, st)
+    _, q, _ = _teacher_entries(z, tau, idx, tl, lse)
+    share = (st[:, 1] / (1.0 + st[:, 1])).abs().nan_to_num(0.0)
+    # ln p in fp64 from an fp32 sum: its error once for every unit of the teacher's mass; the result's rounding
+    tol = q.sum(1) * SUM_TOL * share + 2 * STEP * want.abs().nan_to_num(0, 0, 0) + 1e-12
+    close(loss, want, tol, "loss")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("vocab", [1, 2, 9, 255, 257, 1003, 8191, 8193, 20011])
+def test_distillation(vocab, dtype):
+    z = rows(vocab + 2, KINDS, vocab, dtype)
+    for tau, K, use_lse, tdtype in ((1.0, 8, False, F32), (2.0, 64, True, BF16), (0.7, 1, False, F32), (1.0, 256, True, F32), (4.0, 255, False, BF16)):
+        print(f"distillation V={vocab} {dtype} tau={tau} K={K} lse={use_lse}", flush=True)
+        _check_distill(z, tau, K, use_lse, tdtype, vocab + 1, 1)
+
+
+@pytest.mark.parametrize("T,V", [(1, 151936), (2, 300001), (700, 5003), (1400, 9001)])
+def test_distillation_sizes(T, V):
+    print(f"distillation T={T} V={V}", flush=True)
+    _check_distill(rows(T, ["plain"] * T, V, BF16), 1.0, 40, False)
+
+
+def _distill_gradient(z, tau, idx, tl, lse, d, ld=None, shift=0, ld_d=None, shift_d=0, accumulate=False, in_place=False):
+    T, V = z.shape
+    zd = _to_device(z, ld, shift)
+    _, stats = _distill(zd, tau, idx, tl, lse)
+    out, buf, outside, prior = _gradient_buffers(z, ld_d or V, shift_d, accumulate)
+    if in_place:
+        out = zd
+    remoe.remoe_distill_backward(_desc(V, z.dtype, tau), zd, stats, idx.to(DEV), tl.to(DEV), None if lse is None else lse.to(DEV), d.to(DEV),
+                                 out, accumulate)
+    torch.cuda.synchronize()
+    assert (buf[outside] == 3.0).all(), "written outside the rows"
+    tau = _tau(tau)
+    _, st = oracle.distill(z, tau, idx, tl, lse)
+    want = oracle.distill_grad(z, tau, idx, tl, d, lse)
+    there, q, _ = _teacher_entries(z, tau, idx, tl, lse)
+    mass = q.sum(1, keepdim=True)
+    g = (d.double().abs() / tau)[:, None]
+    tol = grad_tol(z, tau, st, g * mass)
+    # a named token: (e M - q (1 + rest)) / S from the sum, which both products have
+    lp, _ = log_probs(z, tau, st)
+    at = idx.long().clamp(0, V - 1)
+    # in fp64: M is a sum of K terms and M - q a difference, each rounded by up to 2^-53 of M, here and in the oracle, so where
+    # one entry has all but 1e-14 of the mass the difference is known to (K + 8) 2^-52 M and no better
+    tol.scatter_add_(1, at, g * (q * SUM_TOL + mass * (idx.shape[1] + 8) * 2.0 ** -52))
+    _check_gradient(out, want, tol.nan_to_num(0.0), prior if accumulate else None, z.dtype, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("vocab", [1, 2, 9, 257, 1003, 8193, 20011])
+def test_distillation_gradient(vocab, dtype):
+    z = rows(vocab + 3, KINDS, vocab, dtype)
+    d = torch.randn(len(KINDS), generator=torch.Generator().manual_seed(vocab))
+    for i, (tau, K, use_lse, tdtype) in enumerate(((1.0, 8, False, F32), (2.0, 64, True, BF16), (0.7, 1, True, F32), (1.0, 256, False, F32))):
+        print(f"distillation gradient V={vocab} {dtype} K={K} variant {i}", flush=True)
+        idx, tl, lse = _teacher(vocab + K, z, K, tdtype)
+        _distill_gradient(z, tau, idx, tl, lse if use_lse else None, d, accumulate=i == 1, in_place=i == 3)
+
+
+def test_every_entry_names_the_same_token():
+    V, K = 500, 256
+    z = rows(8, ("plain", "peaked"), V, F32)
+    idx = torch.full((2, K), 17, dtype=torch.int32)
+    tl = torch.randn(2, K, generator=torch.Generator().manual_seed(1))
+    _distill_gradient(z, 1.0, idx, tl, None, torch.tensor([1.0, -2.0]))
+
+
+@pytest.mark.parametrize("T,V,dtype", [(2, 151936, BF16), (1, 300001, F32), (700, 5003, BF16), (1400, 9001, BF16)])
+def test_gradient_sizes(T, V, dtype):
+    print(f"gradient sizes T={T} V={V}", flush=True)
+    z = rows(T, ["plain"] * T, V, dtype)
+    g = torch.Generator().manual_seed(T)
+    idx, tl, lse = _teacher(V, z, 33)
+    d = torch.randn(T, generator=g) / T
+    _logprob_gradient(z, 1.0, _targets(T, z), d, d)
+    _distill_gradient(z, 1.0, idx, tl, lse, d)
+
+
+# ---- together -------------------------------------------------------------------------------------
+
+def _training_step(zd, tgt, idx, tl, bufs, desc_ce, desc_kd, T):
+    """Cross-entropy with an entropy bonus and a distillation at another temperature, one gradient."""
+    remoe.remoe_token_logprobs(desc_ce, zd, tgt, bufs["lp"], bufs["h"], bufs["ti"], bufs["tl"], bufs["st"], bufs["ws"])
+    remoe.remoe_distill_forward(desc_kd, zd, idx, tl, None, bufs["kd"], bufs["st2"], bufs["ws2"])
+    remoe.remoe_token_logprobs_backward(desc_ce, zd, bufs["st"], tgt, bufs["g"], bufs["h"], bufs["gh"], bufs["dz"])
+    remoe.remoe_distill_backward(desc_kd, zd, bufs["st2"], idx, tl, None, bufs["gk"], bufs["dz"], accumulate=True)
+
+
+def _training_buffers(z, K, n):
+    T, V = z.shape
+    ce, kd = _desc(V, z.dtype, 1.0), _desc(V, z.dtype, 2.0)
+    bufs = {"lp": _out(T), "h": _out(T), "ti": _out(T, n, dtype=torch.int32), "tl": _out(T, n), "st": _out(T, 2), "kd": _out(T), "st2": _out(T, 2),
+            "ws": _workspace(ce, T, n)[0], "ws2": _workspace(kd, T)[0], "g": torch.full((T,), -0.5, device=DEV),
+            "gh": torch.full((T,), 0.25, device=DEV), "gk": torch.full((T,), 2.0, device=DEV), "dz": torch.empty(T, V, dtype=z.dtype, device=DEV)}
+    return bufs, ce, kd
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_training_step_with_both_losses(dtype):
+    T, V, K = 37, 3001, 16
+    z = rows(21, ["plain"] * T, V, dtype)
+    tgt = _targets(2, z)
+    idx, tl, _ = _teacher(4, z, K)
+    bufs, ce, kd = _training_buffers(z, K, 4)
+    _training_step(_to_device(z), tgt.to(DEV), idx.to(DEV), tl.to(DEV), bufs, ce, kd, T)
+    torch.cuda.synchronize()
+    half, quarter, two = torch.full((T,), -0.5), torch.full((T,), 0.25), torch.full((T,), 2.0)
+    a = oracle.token_logprobs_grad(z, 1.0, tgt, half, quarter)
+    b = oracle.distill_grad(z, 2.0, idx, tl, two)
+    # sums' errors weigh with the largest factor each term can have; two roundings to the tensor's type
+    size = a.abs() + b.abs()
+    _, st = oracle.distill(z, 1.0, idx, tl)
+    tol = (size + 0.5 * torch.exp(log_probs(z, 1.0, st)[0]) + torch.exp(log_probs(z, 2.0, oracle.distill(z, 2.0, idx, tl)[1])[0]) * 2) * 32 * SUM_TOL
+    tol = tol + 2 * (HALF[dtype] + STEP) * size
+    close(bufs["dz"], a + b, tol, "dlogits of both")
+    # the cross-entropy's gradient through torch.autograd in fp64
+    x = z.double().requires_grad_()
+    lp = torch.log_softmax(x, 1)
+    there = (tgt >= 0) & (tgt < V)
+    (lp.gather(1, tgt.long().clamp(0, V - 1)[:, None])[:, 0] * there).sum().backward()
+    assert torch.allclose(oracle.token_logprobs_grad(z, 1.0, tgt, torch.ones(T), None), x.grad, rtol=1e-9, atol=1e-12)
+
+
+def test_captured_and_replayed():
+    """The four calls in a graph, replayed on new logits between eager calls and synchronisations."""
+    T, V, K, n = 5, 40009, 12, 20
+    z = rows(31, ("plain", "masked", "ties", "few", "peaked"), V, BF16)
+    zd, tgt = _to_device(z), _targets(5, z).to(DEV)
+    idx, tl, _ = _teacher(6, z, K)
+    idx, tl = idx.to(DEV), tl.to(DEV)
+    eager, ce, kd = _training_buffers(z, K, n)
+    graphed, _, _ = _training_buffers(z, K, n)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _training_step(zd, tgt, idx, tl, graphed, ce, kd, T)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _training_step(zd, tgt, idx, tl, graphed, ce, kd, T)
+    for i in range(4):
+        zd.copy_(rows(40 + i, ("masked", "plain", "empty", "ties", "peaked"), V, BF16))
+        for k in ("ws", "ws2"):
+            graphed[k].fill_(0xFF)                        # nothing is expected of a workspace
+        _training_step(zd, tgt, idx, tl, eager, ce, kd, T)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in ("lp", "h", "ti", "tl", "st", "kd", "st2", "dz"):
+            assert torch.equal(eager[k].view(torch.int16), graphed[k].view(torch.int16)), (i, k)
+
+
+def test_two_streams_and_repeats():
+    """The same calls on two streams with workspaces of their own give the same bits as one after the other."""
+    T, V, n = 3, 50021, 33
+    z = rows(51, ("plain", "ties", "masked"), V, BF16)
+    zd, tgt = _to_device(z), _targets(7, z)
+    first = _logprobs(zd, 1.0, tgt, n)
+    desc, tgt = _desc(V, BF16, 1.0), tgt.to(DEV)
+    runs = []
+    for s in (torch.cuda.Stream(), torch.cuda.Stream()):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            for _ in range(3):
+                out = (_out(T), _out(T), _out(T, n, dtype=torch.int32), _out(T, n), _out(T, 2))
+                ws = torch.empty(remoe.remoe_head_workspace_bytes(desc, T, n), dtype=torch.uint8, device=DEV)
+                remoe.remoe_token_logprobs(desc, zd, tgt, *out, ws)
+                runs.append((out, ws))
+    torch.cuda.synchronize()
+    for out, _ in runs:
+        for got, want in zip(out, first.values()):
+            assert torch.equal(got.view(torch.int32), want.view(torch.int32))
+
+
+def test_rows_beyond_32_bits():
+    """Rows that start further than 2^31 and 2^32 values into the buffer."""
+    V, ld, T = 1000, (1 << 31) + 7, 3
+    buf = torch.empty(2 * ld + V, dtype=BF16, device=DEV)
+    zd = buf.as_strided((T, V), (ld, 1))
+    z = rows(61, ("plain", "ties", "peaked"), V, BF16)
+    zd.copy_(z)
+    tgt = _targets(9, z)
+    got = _logprobs(zd, 1.0, tgt, 5)
+    _check_logprobs(got, z, 1.0, tgt, 5)
+    desc, g = _desc(V, BF16, 1.0), torch.ones(T)
+    out = torch.empty(T, V, dtype=BF16, device=DEV)
+    remoe.remoe_token_logprobs_backward(desc, zd, got["stats"], tgt.to(DEV), g.to(DEV), None, None, out)
+    remoe.remoe_token_logprobs_backward(desc, zd, got["stats"], tgt.to(DEV), g.to(DEV), None, None, zd)      # in place, far apart
+    torch.cuda.synchronize()
+    assert torch.equal(out.view(torch.int16), zd.contiguous().view(torch.int16))
+    want = oracle.token_logprobs_grad(z, 1.0, tgt, g, None)
+    st = oracle.token_logprobs(z, 1.0, tgt, 0)["stats"]
+    _check_gradient(out, want, grad_tol(z, 1.0, st, torch.ones(T, 1)) + SUM_TOL * want.abs(), None, BF16, "dlogits")
+
+
+def test_the_binding_refuses_wrong_tensors():
+    V = 64
+    desc = _desc(V, BF16, 1.0)
+    z = torch.zeros(4, V, dtype=BF16, device=DEV)
+    st, ws = _out(4, 2), _workspace(desc, 4)[0]
+    i32 = torch.zeros(4, dtype=torch.int32, device=DEV)
+    call = lambda z=z, t=None, lp=None, s=st: remoe.remoe_token_logprobs(desc, z, t, lp, None, None, None, s, ws)
+    call()
+    for kw, word in [(dict(z=z.float()), "logits"), (dict(z=z[:, :32]), "logits"), (dict(z=z.t().contiguous().t()), "follow"), (dict(z=z[0]), "logits"),
+                     (dict(t=i32.long(), lp=_out(4)), "targets"), (dict(t=i32, lp=_out(5)), "out_logprob"), (dict(s=st[:3]), "out_stats"),
+                     (dict(s=_out(2, 4).t()), "contiguous"), (dict(t=i32), "targets"), (dict(z=z[:1].expand(4, V)), "stride")]:
+        with pytest.raises(remoe.RemoeError, match=word):
+            call(**kw)
+    g = _out(4)
+    with pytest.raises(remoe.RemoeError, match="rows"):
+        remoe.remoe_token_logprobs_backward(desc, z, st, i32, g, None, None, z[:3])
+    five = torch.zeros(5, V, dtype=BF16, device=DEV)
+    with pytest.raises(remoe.RemoeError, match="overlaps"):
+        remoe.remoe_token_logprobs_backward(desc, five[:4], st, i32, g, None, None, five[1:])
+    with pytest.raises(remoe.RemoeError, match="teacher_logits"):
+        remoe.remoe_distill_forward(desc, z, i32.view(4, 1), torch.zeros(4, 1, dtype=torch.float16, device=DEV), None, g, None, ws)
+    with pytest.raises(remoe.RemoeError, match="teacher_idx"):
+        remoe.remoe_distill_forward(desc, z, i32, torch.zeros(4, 1, device=DEV), None, g, None, ws)
+    torch.cuda.synchronize()
