@@ -5,97 +5,192 @@
 //
 // A pass over the row writes the terms that every token has; the tokens that are named (the target, the teacher's) are taken
 // from their logits in fp64 and written over it: their differences cancel where the model agrees (1 - p_v, M p_v - q_v).
-// One workgroup per row, an element at a time.
+// A workgroup has a stretch of a row's 16-byte pieces, cut where dlogits is aligned, and all of its named tokens.
 #include "head_rows.h"
 
 namespace remoe {
 
 namespace {
 
-constexpr float LOG2E = 1.44269504088896340736f;
+#ifndef HG_PIECES
+#define HG_PIECES 4
+#endif
+#ifndef HG_WORKGROUPS
+#define HG_WORKGROUPS 4096
+#endif
+constexpr int PIECES = HG_PIECES;      // 16-byte pieces of a thread that are on their way together
 
-template <int DT> __global__ __launch_bounds__(HEAD_THREADS) void head_grad_kernel(const HeadGradArgs a)
+// dz = e * (k0 + k1 x) with x = log2 e, away from the named tokens
+struct RowTerms { float m, c, c_low, k0, k1; };
+
+// e^(d) as 2^x.  fp32 gradients: x to more than fp32 (its product's remainder and the low part of c), since at d = -12 the
+// rounding of x alone would be 20 steps of e; bf16 ones are rounded to 2^-8 anyway.
+template <bool FINE> __device__ __forceinline__ float term(const RowTerms &t, float z)
+{
+    const float d = fmaxf(z - t.m, -512.f / t.c);             // 2^-512 is 0; -inf would make the products below NaN
+    const float x = d * t.c;
+    float e = __builtin_amdgcn_exp2f(x);
+    if constexpr (FINE) e = fmaf(e, 0.693147180559945f * fmaf(d, t.c_low, fmaf(d, t.c, -x)), e);
+    return e * fmaf(t.k1, x, t.k0);
+}
+
+__device__ __forceinline__ void put_one(float *p, float v) { *p = v; }
+__device__ __forceinline__ void put_one(bf16_t *p, float v) { *p = (bf16_t)(pack_bf16x2(v, 0.f) & 0xFFFFu); }
+
+template <int DT, bool TEACHER, bool ADD>
+__global__ __launch_bounds__(HEAD_THREADS) void head_grad_kernel(const HeadGradArgs a, int segs, int seg_pieces)
 {
     typedef typename LogitOf<DT>::type elem;
-    __shared__ double part[HEAD_WAVES];
-    __shared__ int ids[HEAD_THREADS];
-    __shared__ double qs[HEAD_THREADS];
-    const int64_t row = blockIdx.x;
+    typedef Piece<DT> P;
+    constexpr bool FINE = DT == REMOE_F32;
+    const int64_t row = blockIdx.x / (unsigned)segs;
+    const int seg = blockIdx.x % (unsigned)segs;
     const int tid = threadIdx.x, V = a.V;
     const elem *z = static_cast<const elem *>(a.logits) + row * a.ld;
     elem *dz = static_cast<elem *>(a.dlogits) + row * a.ld_d;
-    const float m = a.stats[2 * row], rest = a.stats[2 * row + 1];
-    const float c = LOG2E / a.tau, inv_s = 1.f / (1.f + rest);
-    const bool empty = rest == -1.f;
+    // values in front of the first aligned piece of dlogits, whole pieces, values behind the last
+    int head = (int)((16 - ((uintptr_t)dz & 15)) & 15) / (int)sizeof(elem);
+    if (head > V) head = V;
+    const int pieces = (V - head) / P::N;
+    const int p0 = seg * seg_pieces, p1 = seg == segs - 1 || p0 + seg_pieces > pieces ? pieces : p0 + seg_pieces;
+    const int v0 = seg == 0 ? 0 : head + p0 * P::N, v1 = seg == segs - 1 ? V : head + p1 * P::N;      // this workgroup's values
 
-    // coefficients: dz = p * (k0 + k1 * d) away from the named tokens
+    // the first pieces are on their way while the row's terms are put together
+    const elem *zp = z + head;
+    elem *dp = dz + head;
+    u32x4_t in[PIECES], old[ADD ? PIECES : 1];
+    auto request = [&](int p) {
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u) {
+            const int at = p + u * HEAD_THREADS;
+            if (at < p1) {
+                in[u] = *reinterpret_cast<const u32x4_any_t *>(zp + (int64_t)at * P::N);
+                if constexpr (ADD) old[u] = *reinterpret_cast<const u32x4_t *>(dp + (int64_t)at * P::N);
+            }
+        }
+    };
+    request(p0 + tid);
+
+    const float m = a.stats[2 * row], rest = a.stats[2 * row + 1];
+    const bool empty = rest == -1.f;
+    RowTerms t;
+    {
+        const double c = 1.4426950408889634074 / (double)a.tau;
+        t.c = (float)c;
+        t.c_low = (float)(c - (double)t.c);
+    }
+    t.m = empty ? 0.f : m;
+    const float inv_s = empty ? 0.f : 1.f / (1.f + rest);
+    t.k0 = t.k1 = 0.f;
     int named = -1;
     double q = 0.0, mass = 0.0;
-    float k0, k1 = 0.f, h = 0.f;
-    if (a.teacher_idx) {
-        const TeacherEntry e = teacher_entry(a.teacher_idx, a.teacher_logits, a.teacher_dtype, a.teacher_lse, a.K, V, a.tau, row, part);
+    if constexpr (TEACHER) {
+        __shared__ double part[HEAD_WAVES];
+        __shared__ __align__(16) int ids[HEAD_THREADS];
+        __shared__ double qs[HEAD_THREADS];
+        const TeacherEntry e = teacher_entry<true>(a.teacher_idx, a.teacher_logits, a.teacher_dtype, a.teacher_lse, a.K, V, a.tau, row, part);
         named = e.id;
         q = e.q;
-        mass = block_reduce(q, part, OpSum());
-        k0 = (float)((double)a.d_loss[row] * mass / (double)a.tau);
+        mass = e.mass;
+        t.k0 = (float)((double)a.d_loss[row] * mass / (double)a.tau) * inv_s;
         ids[tid] = named;
         qs[tid] = q;
         __syncthreads();
+        if (named < v0 || named >= v1) named = -1;
         if (named >= 0)                  // an id that stands there more than once: its first entry takes them all
-            for (int j = 0; j < a.K; ++j)
-                if (j != tid && ids[j] == named) {
-                    if (j < tid) { named = -1; break; }
-                    q += qs[j];
-                }
+            for (int j = 0; j < a.K && named >= 0; j += 4) {     // (threads behind K have id -1)
+                const int4 four = *reinterpret_cast<const int4 *>(ids + j);
+                const int id[4] = {four.x, four.y, four.z, four.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (id[i] == e.id && j + i != tid) {
+                        if (j + i < tid) named = -1;
+                        else q += qs[j + i];
+                    }
+            }
     } else {
-        const int t = a.targets ? a.targets[row] : -1;
-        const float g = t >= 0 && t < V ? a.d_logprob[row] : 0.f;
-        if (tid == 0 && t >= 0 && t < V) named = t;
-        k0 = -g / a.tau;
-        if (a.d_entropy) {
-            h = a.d_entropy[row] / a.tau;
+        const int target = a.targets ? a.targets[row] : -1;
+        const bool there = target >= 0 && target < V;
+        const float g = there ? a.d_logprob[row] : 0.f;
+        if (tid == 0 && target >= v0 && target < v1) named = target;
+        float k0 = -g / a.tau;
+        if (a.d_entropy && !empty) {
+            const float h = a.d_entropy[row] / a.tau;
             k0 -= h * (a.entropy[row] - log1pf(rest));
-            k1 = -h;
+            t.k1 = -h * 0.693147180559945f * inv_s;
         }
+        t.k0 = k0 * inv_s;
     }
-    auto at = [&](float zv) {
-        const float x = (zv - m) * c, e = __builtin_amdgcn_exp2f(x);
-        float v = e * inv_s * k0;
-        if (k1 != 0.f && e > 0.f) v += e * inv_s * (k1 * (x * (1.f / LOG2E)));
-        return empty ? 0.f : v;
-    };
     // the named token's value, before the pass below may write over its logit
     float exact = 0.f;
     if (named >= 0) {
-        const float zv = widen(z[named]);
         if (!empty) {
-            const double d = ((double)zv - (double)m) / (double)a.tau, s = 1.0 + (double)rest;
+            const double d = ((double)widen(z[named]) - (double)m) / (double)a.tau, s = 1.0 + (double)rest;
             double v;
-            if (a.teacher_idx) v = (double)a.d_loss[row] * ((expm1(d) * mass + (mass - q) - q * (double)rest) / s);
+            if constexpr (TEACHER) v = (double)a.d_loss[row] * ((expm1(d) * mass + (mass - q) - q * (double)rest) / s);
             else {
-                v = (double)a.d_logprob[row] * (((double)rest - expm1(d)) / s);
+                v = a.d_logprob ? (double)a.d_logprob[row] * (((double)rest - expm1(d)) / s) : 0.0;
                 if (a.d_entropy && exp(d) > 0.0) v -= (double)a.d_entropy[row] * (exp(d) / s) * (d - log1p((double)rest) + (double)a.entropy[row]);
             }
             exact = (float)(v / (double)a.tau);
         }
-        if (a.accumulate) exact += widen(dz[named]);
+        if (ADD) exact += widen(dz[named]);
     }
-    auto store = [&](int v, float f) {
-        if constexpr (DT == REMOE_BF16) dz[v] = (bf16_t)(pack_bf16x2(f, 0.f) & 0xFFFFu);
-        else dz[v] = f;
-    };
     __syncthreads();
-    for (int v = tid; v < V; v += HEAD_THREADS) store(v, at(widen(z[v])) + (a.accumulate ? widen(dz[v]) : 0.f));
+
+    // the values outside whole pieces, one to a thread
+    {
+        const int behind = head + pieces * P::N;
+        int v = -1;
+        if (seg == 0 && tid < head) v = tid;
+        if (seg == segs - 1 && tid >= 64 && tid - 64 < V - behind) v = behind + tid - 64;
+        if (v >= 0) put_one(dz + v, term<FINE>(t, widen(z[v])) + (ADD ? widen(dz[v]) : 0.f));
+    }
+    for (int p = p0 + tid; p < p1; p += PIECES * HEAD_THREADS) {
+        u32x4_t now[PIECES], add[ADD ? PIECES : 1];
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u) {
+            now[u] = in[u];
+            if constexpr (ADD) add[u] = old[u];
+        }
+        request(p + PIECES * HEAD_THREADS);
+#pragma unroll
+        for (int u = 0; u < PIECES; ++u) {
+            if (p + u * HEAD_THREADS >= p1) break;
+            float v[P::N], w[P::N];
+            P::get(now[u], v);
+            if constexpr (ADD) P::get(add[u], w);
+#pragma unroll
+            for (int i = 0; i < P::N; ++i) v[i] = ADD ? term<FINE>(t, v[i]) + w[i] : term<FINE>(t, v[i]);
+            __builtin_nontemporal_store(P::put(v), reinterpret_cast<u32x4_t *>(dp + (int64_t)(p + u * HEAD_THREADS) * P::N));
+        }
+    }
     __syncthreads();
-    if (named >= 0) store(named, exact);
+    if (named >= 0) put_one(dz + named, exact);
 }
 
 }  // namespace
 
 remoe_status launch_head_backward(const HeadGradArgs &a, hipStream_t stream)
 {
-    const dim3 grid((unsigned)a.T), block(HEAD_THREADS);
-    hipLaunchKernelGGL(a.dtype == REMOE_BF16 ? head_grad_kernel<REMOE_BF16> : head_grad_kernel<REMOE_F32>, grid, block, 0, stream, a);
+    const int per = a.dtype == REMOE_BF16 ? 8 : 4;
+    const int64_t pieces = ceil_div(a.V, per);
+    int64_t segs = ceil_div(HG_WORKGROUPS, a.T);
+    const int64_t most = ceil_div(pieces, HEAD_THREADS);
+    if (segs > most) segs = most;
+    const int seg_pieces = (int)ceil_div(pieces, segs);
+    segs = ceil_div(pieces, seg_pieces);
+    auto kernel = [&]() {
+        const bool bf16 = a.dtype == REMOE_BF16;
+        if (a.teacher_idx) {
+            if (a.accumulate) return bf16 ? head_grad_kernel<REMOE_BF16, true, true> : head_grad_kernel<REMOE_F32, true, true>;
+            return bf16 ? head_grad_kernel<REMOE_BF16, true, false> : head_grad_kernel<REMOE_F32, true, false>;
+        }
+        if (a.accumulate) return bf16 ? head_grad_kernel<REMOE_BF16, false, true> : head_grad_kernel<REMOE_F32, false, true>;
+        return bf16 ? head_grad_kernel<REMOE_BF16, false, false> : head_grad_kernel<REMOE_F32, false, false>;
+    }();
+    const dim3 grid((unsigned)(a.T * segs)), block(HEAD_THREADS);
+    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, (int)segs, seg_pieces);
     return check_hip(hipGetLastError(), "head gradient kernel launch");
 }
 
