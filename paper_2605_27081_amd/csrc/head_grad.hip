@@ -13,11 +13,12 @@ namespace remoe {
 namespace {
 
 #ifndef HG_PIECES
-#define HG_PIECES 4
+#define HG_PIECES 2
 #endif
 #ifndef HG_WORKGROUPS
-#define HG_WORKGROUPS 4096
+#define HG_WORKGROUPS 8192
 #endif
+constexpr int NT = 256;
 constexpr int PIECES = HG_PIECES;      // 16-byte pieces of a thread that are on their way together
 
 // dz = e * (k0 + k1 x) with x = log2 e, away from the named tokens
@@ -38,7 +39,7 @@ __device__ __forceinline__ void put_one(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put_one(bf16_t *p, float v) { *p = (bf16_t)(pack_bf16x2(v, 0.f) & 0xFFFFu); }
 
 template <int DT, bool TEACHER, bool ADD>
-__global__ __launch_bounds__(HEAD_THREADS) void head_grad_kernel(const HeadGradArgs a, int segs, int seg_pieces)
+__global__ __launch_bounds__(NT) void head_grad_kernel(const HeadGradArgs a, int segs, int seg_pieces)
 {
     typedef typename LogitOf<DT>::type elem;
     typedef Piece<DT> P;
@@ -59,10 +60,10 @@ __global__ __launch_bounds__(HEAD_THREADS) void head_grad_kernel(const HeadGradA
     const elem *zp = z + head;
     elem *dp = dz + head;
     u32x4_t in[PIECES], old[ADD ? PIECES : 1];
-    auto request = [&](int p) {
+    auto request = [&](int p) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) {
-            const int at = p + u * HEAD_THREADS;
+            const int at = p + u * NT;
             if (at < p1) {
                 in[u] = *reinterpret_cast<const u32x4_any_t *>(zp + (int64_t)at * P::N);
                 if constexpr (ADD) old[u] = *reinterpret_cast<const u32x4_t *>(dp + (int64_t)at * P::N);
@@ -85,10 +86,10 @@ __global__ __launch_bounds__(HEAD_THREADS) void head_grad_kernel(const HeadGradA
     int named = -1;
     double q = 0.0, mass = 0.0;
     if constexpr (TEACHER) {
-        __shared__ double part[HEAD_WAVES];
-        __shared__ __align__(16) int ids[HEAD_THREADS];
-        __shared__ double qs[HEAD_THREADS];
-        const TeacherEntry e = teacher_entry<true>(a.teacher_idx, a.teacher_logits, a.teacher_dtype, a.teacher_lse, a.K, V, a.tau, row, part);
+        __shared__ double part[NT / 64];
+        __shared__ __align__(16) int ids[NT];
+        __shared__ double qs[NT];
+        const TeacherEntry e = teacher_entry<NT, true>(a.teacher_idx, a.teacher_logits, a.teacher_dtype, a.teacher_lse, a.K, V, a.tau, row, part);
         named = e.id;
         q = e.q;
         mass = e.mass;
@@ -146,23 +147,23 @@ __global__ __launch_bounds__(HEAD_THREADS) void head_grad_kernel(const HeadGradA
         if (seg == segs - 1 && tid >= 64 && tid - 64 < V - behind) v = behind + tid - 64;
         if (v >= 0) put_one(dz + v, term<FINE>(t, widen(z[v])) + (ADD ? widen(dz[v]) : 0.f));
     }
-    for (int p = p0 + tid; p < p1; p += PIECES * HEAD_THREADS) {
+    for (int p = p0 + tid; p < p1; p += PIECES * NT) {
         u32x4_t now[PIECES], add[ADD ? PIECES : 1];
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) {
             now[u] = in[u];
             if constexpr (ADD) add[u] = old[u];
         }
-        request(p + PIECES * HEAD_THREADS);
+        request(p + PIECES * NT);
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) {
-            if (p + u * HEAD_THREADS >= p1) break;
+            if (p + u * NT >= p1) break;
             float v[P::N], w[P::N];
             P::get(now[u], v);
             if constexpr (ADD) P::get(add[u], w);
 #pragma unroll
             for (int i = 0; i < P::N; ++i) v[i] = ADD ? term<FINE>(t, v[i]) + w[i] : term<FINE>(t, v[i]);
-            __builtin_nontemporal_store(P::put(v), reinterpret_cast<u32x4_t *>(dp + (int64_t)(p + u * HEAD_THREADS) * P::N));
+            __builtin_nontemporal_store(P::put(v), reinterpret_cast<u32x4_t *>(dp + (int64_t)(p + u * NT) * P::N));
         }
     }
     __syncthreads();
@@ -176,7 +177,7 @@ remoe_status launch_head_backward(const HeadGradArgs &a, hipStream_t stream)
     const int per = a.dtype == REMOE_BF16 ? 8 : 4;
     const int64_t pieces = ceil_div(a.V, per);
     int64_t segs = ceil_div(HG_WORKGROUPS, a.T);
-    const int64_t most = ceil_div(pieces, HEAD_THREADS);
+    const int64_t most = ceil_div(pieces, NT);
     if (segs > most) segs = most;
     const int seg_pieces = (int)ceil_div(pieces, segs);
     segs = ceil_div(pieces, seg_pieces);
@@ -189,7 +190,7 @@ remoe_status launch_head_backward(const HeadGradArgs &a, hipStream_t stream)
         if (a.accumulate) return bf16 ? head_grad_kernel<REMOE_BF16, false, true> : head_grad_kernel<REMOE_F32, false, true>;
         return bf16 ? head_grad_kernel<REMOE_BF16, false, false> : head_grad_kernel<REMOE_F32, false, false>;
     }();
-    const dim3 grid((unsigned)(a.T * segs)), block(HEAD_THREADS);
+    const dim3 grid((unsigned)(a.T * segs)), block(NT);
     hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, (int)segs, seg_pieces);
     return check_hip(hipGetLastError(), "head gradient kernel launch");
 }

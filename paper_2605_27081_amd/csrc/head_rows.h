@@ -1,13 +1,10 @@
 // What the kernels over the vocabulary share (head.hip, head_grad.hip): reading a logit, sums and maxima over a workgroup,
-// a teacher's list.  Workgroups have HEAD_THREADS threads throughout.
+// a teacher's list.  NT is the number of threads of a workgroup.
 #pragma once
 
 #include "common.h"
 
 namespace remoe {
-
-constexpr int HEAD_THREADS = 256;
-constexpr int HEAD_WAVES = HEAD_THREADS / 64;
 
 template <int DT> struct LogitOf;
 template <> struct LogitOf<REMOE_F32> { typedef float type; };
@@ -23,8 +20,8 @@ template <typename V, typename Op> __device__ __forceinline__ V wave_reduce(V v,
     return v;
 }
 
-// over the workgroup, the same value in every thread, in a fixed order; `part` is HEAD_WAVES values of LDS
-template <typename V, typename Op> __device__ __forceinline__ V block_reduce(V v, V *part, Op op)
+// over the workgroup, the same value in every thread, in a fixed order; `part` is a value of LDS for every wavefront
+template <int NT, typename V, typename Op> __device__ __forceinline__ V block_reduce(V v, V *part, Op op)
 {
     v = wave_reduce(v, op);
     __syncthreads();                    // the previous use of part is over
@@ -32,19 +29,19 @@ template <typename V, typename Op> __device__ __forceinline__ V block_reduce(V v
     __syncthreads();
     V r = part[0];
 #pragma unroll
-    for (int w = 1; w < HEAD_WAVES; ++w) r = op(r, part[w]);
+    for (int w = 1; w < NT / 64; ++w) r = op(r, part[w]);
     return r;
 }
 
 struct OpSum { template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a + b; } };
 struct OpMax { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 
-// One entry of a teacher's list, thread j holds entry j: q_j and ln q_j in fp64 (a few values per row, and they are
+// One entry of a teacher's list, thread j holds entry j (K <= NT): q_j and ln q_j in fp64 (a few values per row, and they are
 // subtracted from the model's own).  Entries that are absent have id -1 and q 0.  mass = sum_j q_j: 1 by definition where the
 // list is normalised by itself and not empty, and only formed where MASS is set.
 struct TeacherEntry { int id; double q, log_q, mass; };
 
-template <bool MASS>
+template <int NT, bool MASS>
 __device__ __forceinline__ TeacherEntry teacher_entry(const int32_t *idx, const void *logits, int dtype, const float *lse, int K, int V,
                                                       float tau, int64_t row, double *part)
 {
@@ -63,12 +60,12 @@ __device__ __forceinline__ TeacherEntry teacher_entry(const int32_t *idx, const 
             e.log_q = (double)t / (double)tau - (double)lse[row];
             e.q = exp(e.log_q);
         }
-        if constexpr (MASS) e.mass = block_reduce(e.q, part, OpSum());
+        if constexpr (MASS) e.mass = block_reduce<NT>(e.q, part, OpSum());
     } else {
-        const float top = block_reduce(t, reinterpret_cast<float *>(part), OpMax());
+        const float top = block_reduce<NT>(t, reinterpret_cast<float *>(part), OpMax());
         const double d = e.id >= 0 ? ((double)t - (double)top) / (double)tau : 0.0;
         const double q = e.id >= 0 ? exp(d) : 0.0;
-        const double sum = block_reduce(q, part, OpSum());
+        const double sum = block_reduce<NT>(q, part, OpSum());
         if (e.id >= 0) {
             e.q = q / sum;
             e.log_q = d - log(sum);
