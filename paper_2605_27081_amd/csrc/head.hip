@@ -9,9 +9,9 @@
 // logit's own 1, which a running sum cannot take back: the thread that has the largest logit has its pieces read once more (a
 // piece per thread of the workgroup).
 //
-// Alternatives: the n-th largest of the threads' maxima is a bound that at least n logits reach, and not many more do, so the
-// maxima of every 32 logits are kept in LDS; those that reach the bound have their pieces read again, and the logits found are
-// ranked by counting the larger ones.  Where too many reach it (ties by the thousand: a mask that leaves fewer than n tokens), or
+// Alternatives: every wavefront has a bound that n / wavefronts of its lanes' maxima reach, so n logits of the row reach the
+// least of the bounds, and not many more do.  The maxima of every 32 logits are kept in LDS; those that reach it have their pieces
+// read again, and the logits found are ranked by counting the larger ones.  Where too many reach it (ties by the thousand: a mask that leaves fewer than n tokens), or
 // the row holds NaN, every wavefront keeps a sorted list, an entry per lane, over a quarter of the row.
 //
 // Few rows are cut into parts; head_join_kernel puts the parts together.
@@ -22,32 +22,24 @@ namespace remoe {
 
 namespace {
 
-#ifndef HS_WORKGROUPS
-#define HS_WORKGROUPS 2048
-#endif
-#ifndef HS_NT
-#define HS_NT 256
-#endif
-#ifndef HS_MIN_UNITS
-#define HS_MIN_UNITS 2
-#endif
-
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
 constexpr float LOWEST = -3.402823466e38f;
 constexpr int BATCH = 32;                               // logits of a thread that are taken together
-constexpr int MAX_PART = 1 << 18;                       // logits of a part: 8192 batches
+constexpr int MAX_BATCHES = 32;                         // of a thread: bits of a mask
+constexpr int64_t MAX_PART = 1 << 18;                   // logits of a part
 constexpr int MAX_PARTS = 64;                           // a lane each in the join
 constexpr int MAX_N = 64;
-constexpr int FOUND = 1024;                             // logits that may reach the bound
+constexpr int FOUND = 512;                              // logits that may reach the bound
 
 // what the logits of a row, or of a part of it, add up to: largest, sum of the e^d without one of the largest, sum of x 2^x
 // (x = log2 e d)
 struct RowSums { float m, rest, xsum; };
 
-__device__ __forceinline__ float log_p(const RowSums &r, float z, float tau)
+// ln p of a logit; log_s = log1p(rest).  (Code that a row passes once is kept short throughout: few rows find none of it in the
+// instruction cache, and 64 bytes of it cost 100 cycles then.)
+__device__ __forceinline__ float log_p(const RowSums &r, float log_s, float z, float tau)
 {
-    if (r.rest == -1.f) return -__builtin_inff();            // nothing but -inf
-    return (z - r.m) / tau - log1pf(r.rest);
+    return r.rest == -1.f ? -__builtin_inff() : (z - r.m) / tau - log_s;      // (-1: nothing but -inf)
 }
 
 // Order of the alternatives: larger logits first, NaN above all, the lower id first among equals.
@@ -70,33 +62,33 @@ struct Rescale {
     __device__ __forceinline__ Rescale(float from, float to, float c) : dx(fmaxf((from - to) * c, -512.f)), f(__builtin_amdgcn_exp2f(dx)) {}
 };
 
-// The outputs of a row by its workgroup, from its sums.  target, target_z: its token and that one's logit.
-template <int NT, typename elem>
-__device__ __forceinline__ void finish_row(const HeadArgs &a, int64_t row, const elem *z, const RowSums &r, int target, float target_z, double *part)
+// The outputs of a row that one thread writes, from its sums.  target, target_z: its token and that one's logit.
+__device__ __forceinline__ void finish_row(const HeadArgs &a, int64_t row, const RowSums &r, float log_s, int target, float target_z)
 {
-    const int tid = threadIdx.x;
-    if (tid == 0) {
-        if (a.stats) {
-            a.stats[2 * row] = r.m;
-            a.stats[2 * row + 1] = r.rest;
-        }
-        if (a.targets) a.logprob[row] = target >= 0 && target < a.V ? log_p(r, target_z, a.tau) : 0.f;
-        if (a.entropy) {
-            const float h = r.rest == -1.f ? 0.f : log1pf(r.rest) - r.xsum * LN2 / (1.f + r.rest);
-            a.entropy[row] = h < 0.f ? 0.f : h;
-        }
+    if (a.stats) {
+        a.stats[2 * row] = r.m;
+        a.stats[2 * row + 1] = r.rest;
     }
-    if (a.teacher_idx) {
-        const TeacherEntry e = teacher_entry<NT, false>(a.teacher_idx, a.teacher_logits, a.teacher_dtype, a.teacher_lse, a.K, a.V, a.tau, row, part);
-        double term = 0.0;
-        if (e.q != 0.0) {
-            const double lp = r.rest == -1.f ? -(double)__builtin_inff()
-                                             : ((double)widen(z[e.id]) - (double)r.m) / (double)a.tau - log1p((double)r.rest);
-            term = e.q * (e.log_q - lp);
-        }
-        const double loss = block_reduce<NT>(term, part, OpSum());
-        if (tid == 0) a.loss[row] = r.rest != r.rest ? r.rest : (float)loss;
+    if (a.targets) a.logprob[row] = target >= 0 && target < a.V ? log_p(r, log_s, target_z, a.tau) : 0.f;
+    if (a.entropy) {
+        const float h = r.rest == -1.f ? 0.f : log_s - r.xsum * LN2 / (1.f + r.rest);
+        a.entropy[row] = h < 0.f ? 0.f : h;
     }
+}
+
+// The divergence from the teacher's list, by a workgroup of at least K threads.
+template <int NT, typename elem>
+__device__ __forceinline__ void finish_teacher(const HeadArgs &a, int64_t row, const elem *z, const RowSums &r, double *part)
+{
+    const TeacherEntry e = teacher_entry<NT, false>(a.teacher_idx, a.teacher_logits, a.teacher_dtype, a.teacher_lse, a.K, a.V, a.tau, row, part);
+    double term = 0.0;
+    if (e.q != 0.0) {
+        const double lp = r.rest == -1.f ? -(double)__builtin_inff()
+                                         : ((double)widen(z[e.id]) - (double)r.m) / (double)a.tau - log1p((double)r.rest);
+        term = e.q * (e.log_q - lp);
+    }
+    const double loss = block_reduce<NT>(term, part, OpSum());
+    if (threadIdx.x == 0) a.loss[row] = r.rest != r.rest ? r.rest : (float)loss;
 }
 
 // The token of a row and its logit, asked for ahead of their use (by every thread: the token is a scalar load then).
@@ -107,23 +99,15 @@ template <typename elem> __device__ __forceinline__ void request_target(const He
     if (target >= 0 && target < a.V) target_z = widen(z[target]);
 }
 
-// A bound that at least n of the EACH x 64 values of a wavefront reach, and no more than a quarter more than n where values
-// differ enough: bisection between the smallest and the largest.
-template <int EACH, typename U> __device__ __forceinline__ U bound_of(const U *value, int n)
+// A bound that at least n of a wavefront's values, one a lane, reach, and no more than a quarter more than n where they differ
+// enough: bisection between the smallest and the largest.
+__device__ __forceinline__ uint32_t bound_of(uint32_t value, int n)
 {
-    U least = value[0], most = value[0];
-#pragma unroll
-    for (int i = 1; i < EACH; ++i) {
-        least = value[i] < least ? value[i] : least;
-        most = value[i] > most ? value[i] : most;
-    }
-    U lo = wave_reduce(least, [](U a, U b) { return a < b ? a : b; });                // all reach it
-    U hi = wave_reduce(most, [](U a, U b) { return a > b ? a : b; }) + 1;             // none does
+    uint32_t lo = wave_min_u32(value);                        // all reach it
+    uint32_t hi = ~wave_min_u32(~value) + 1;                  // none does
     while (hi - lo > 1) {
-        const U mid = lo + (hi - lo) / 2;
-        int reach = 0;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) reach += __popcll(__ballot(value[i] >= mid));
+        const uint32_t mid = lo + (hi - lo) / 2;
+        const int reach = __popcll(__ballot(value >= mid));
         if (reach < n) hi = mid;
         else {
             lo = mid;
@@ -154,36 +138,72 @@ template <int NT, typename Emit> __device__ __forceinline__ void ranked(const ui
     }
 }
 
-// The n largest keys of a stretch of values, by a wavefront: lane i holds the i-th.  Any order of the values will do.
-template <int DT>
-__device__ __forceinline__ uint64_t sorted_list(const typename LogitOf<DT>::type *z, int first, int last, int n)
+// A sorted list of a wavefront's n largest keys, lane i holds the i-th.  Any order of the keys will do.
+struct SortedList {
+    uint64_t mine = 0, least = 0;                             // least: the n-th, which a key has to exceed
+
+    __device__ __forceinline__ static uint64_t from_lane(uint64_t v, int lane)
+    {
+        return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)v, lane);
+    }
+    __device__ __forceinline__ static uint64_t from_left(uint64_t v)          // the lane below's (DPP wave_shr:1)
+    {
+        const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), 0x138, 0xF, 0xF, false);
+        const int lo = __builtin_amdgcn_update_dpp(0, (int)v, 0x138, 0xF, 0xF, false);
+        return (uint64_t)(uint32_t)hi << 32 | (uint32_t)lo;
+    }
+    // a key of every lane (0: none)
+    __device__ __forceinline__ void offer(uint64_t key, int n)
+    {
+        const int lane = threadIdx.x & 63;
+        uint64_t better = __ballot(key > least);
+        while (better) {
+            const int l = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)better) - 1);
+            const uint64_t k = from_lane(key, l);
+            const int at = __popcll(__ballot(mine > k));
+            const uint64_t below = from_left(mine);
+            mine = lane < at ? mine : lane == at ? k : below;
+            least = from_lane(mine, n - 1);
+            better &= better - 1;
+            better &= __ballot(key > least);
+        }
+    }
+};
+
+// The list of pieces [p0, p1); the first value of the first piece of zp has the id id0.
+template <int DT> __device__ __forceinline__ void offer_pieces(SortedList &list, const typename LogitOf<DT>::type *zp, int id0, int p0, int p1, int n)
 {
-    constexpr int N = 8;                                      // values of a lane that are on their way together
+    typedef Piece<DT> P;
+    constexpr int FLIGHT = 4;                                 // pieces of a lane that are on their way together
     const int lane = threadIdx.x & 63;
-    uint64_t mine = 0, least = 0;
-    for (int v = first; v < last; v += 64 * N) {
-        uint64_t key[N];
+    for (int p = p0 + lane; p - lane < p1; p += 64 * FLIGHT) {
+        u32x4_t in[FLIGHT];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int at = v + 64 * i + lane;
-            key[i] = at < last ? rank_key(widen(z[at]), at) : 0;
+        for (int u = 0; u < FLIGHT; ++u) {
+            in[u] = P::lowest();
+            if (p + 64 * u < p1) in[u] = *reinterpret_cast<const u32x4_t *>(zp + (int64_t)(p + 64 * u) * P::N);
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            uint64_t better = __ballot(key[i] > least);
-            while (better) {
-                const int l = __ffsll((unsigned long long)better) - 1;
-                const uint64_t k = __shfl(key[i], l, 64);
-                const int at = __popcll(__ballot(mine > k));
-                const uint64_t above = __shfl_up(mine, 1, 64);
-                mine = lane < at ? mine : lane == at ? k : above;
-                least = __shfl(mine, n - 1, 64);
-                better &= better - 1;
-                better &= __ballot(key[i] > least);
+        for (int u = 0; u < FLIGHT; ++u) {
+            const bool there = p + 64 * u < p1;
+            const int id = id0 + (p + 64 * u) * P::N;
+            const float least = value_of((uint32_t)(list.least >> 32));       // NaN at first: nothing is below it
+            const bool behind = id > key_id(list.least);                      // equals come too late
+            float v[P::N];
+            P::get(in[u], v);
+            bool some = false;
+#pragma unroll
+            for (int k = 0; k < P::N; ++k) some |= behind ? !(v[k] <= least) : !(v[k] < least);
+            if (!__ballot(there && some)) continue;
+#pragma unroll 1
+            for (int k = 0; k < P::N; ++k) {
+                float vk = v[0];
+#pragma unroll
+                for (int i = 1; i < P::N; ++i) vk = k == i ? v[i] : vk;
+                list.offer(there ? rank_key(vk, id + k) : 0, n);
             }
         }
     }
-    return mine;
 }
 
 struct PartOut {              // a part's results in the workspace
@@ -191,16 +211,19 @@ struct PartOut {              // a part's results in the workspace
     uint64_t *keys;           // [T, parts, n], descending, 0 where there are fewer
 };
 
-template <int NT, int DT, bool ENTROPY, bool TOP>
+template <int NT, int DT, bool ENTROPY, bool TOP, bool TEACHER>
 __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int parts, int part_len, PartOut out)
 {
     typedef typename LogitOf<DT>::type elem;
     typedef Piece<DT> P;
-    constexpr int PIECES = BATCH / P::N, WAVES = NT / 64;
+    constexpr int PIECES = BATCH / P::N, WORDS = PIECES * 4, WAVES = NT / 64;
     extern __shared__ float block_max[];                      // [batches + 1, threads]: the maxima of every 32 logits
-    __shared__ double part[WAVES];
+    __shared__ double part[TEACHER ? WAVES : 1];
     __shared__ float wave_m[WAVES], sums[3][WAVES];
-    __shared__ int wave_first[WAVES];
+    __shared__ int wave_first[WAVES], n_found, n_blocks;
+    __shared__ uint16_t blocks[TOP ? FOUND : 1];
+    __shared__ uint32_t wave_bound[WAVES];
+    __shared__ uint64_t found[TOP ? FOUND : 1];
     const int64_t row = blockIdx.x / (unsigned)parts;
     const int p = blockIdx.x % (unsigned)parts;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -236,14 +259,10 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
     float m = edge, ref = fmaxf(edge, LOWEST), s = 0.f, xs = 0.f;
     if (edge_at >= 0) s = __builtin_amdgcn_exp2f((edge - ref) * c);
     if constexpr (TOP) block_max[batches * NT + tid] = edge;
-    u32x4_t last[PIECES];
     for (int b = 0; b < batches; ++b) {
         float v[BATCH];
 #pragma unroll
-        for (int u = 0; u < PIECES; ++u) {
-            last[u] = next[u];
-            P::get(last[u], v + u * P::N);
-        }
+        for (int u = 0; u < PIECES; ++u) P::get(next[u], v + u * P::N);
         if (b + 1 < batches) request(b + 1);
         float bm = v[0];
 #pragma unroll
@@ -266,16 +285,19 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
         if constexpr (ENTROPY) xs += (x4[0] + x4[1]) + (x4[2] + x4[3]);
     }
 
-    // the largest logit and the first thread that has it
-    __shared__ float thread_m[TOP ? NT : 1];
-    if constexpr (TOP) thread_m[tid] = m;
+    // the largest logit and the first thread that has it; a bound that n threads' maxima reach, if n / WAVES of every wavefront do
     {
         const float wm = wave_max(m);
         const uint64_t has = __ballot(m == wm);
+        uint32_t reached = 0;
+        if constexpr (TOP) reached = bound_of(order_of(m), (a.top_n + WAVES - 1) / WAVES);
         if (lane == 0) {
             wave_m[wave] = wm;
             wave_first[wave] = has ? __ffsll((unsigned long long)has) - 1 : 0;
+            if constexpr (TOP) wave_bound[wave] = reached;
         }
+        if constexpr (TOP)
+            if (tid == 0) n_found = n_blocks = 0;
     }
     __syncthreads();
     float top = wave_m[0];
@@ -287,60 +309,56 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
             owner = w * 64 + wave_first[w];
         }
     const float to = fmaxf(top, LOWEST);
+    u32x4_t own = P::lowest();                                // a piece of the owner's
+    if (tid * NT + owner < pieces) own = *reinterpret_cast<const u32x4_t *>(zp + (int64_t)(tid * NT + owner) * P::N);
+    float least = 0.f;                                        // logits that reach it may be alternatives
+    if constexpr (TOP) {
+        uint32_t l = wave_bound[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) l = min(l, wave_bound[w]);
+        least = value_of(l);
+        // this thread's blocks of 32 that hold some (the last ones may be nothing but padding)
+        if (m >= least) {
+            uint32_t hits = 0;
+#pragma unroll 4
+            for (int b = 0; b < batches; ++b) hits |= (block_max[b * NT + tid] >= least && b * PIECES * NT + tid < pieces ? 1u : 0u) << b;
+            while (hits) {
+                const int b = __ffs(hits) - 1, at = atomicAdd(&n_blocks, 1);
+                hits &= hits - 1;
+                if (at < FOUND) blocks[at] = (uint16_t)(b * NT + tid);
+            }
+            if (edge_at >= 0 && edge >= least) {
+                const int at = atomicAdd(&n_found, 1);
+                if (at < FOUND) found[at] = rank_key(edge, v0 + edge_at);
+            }
+        }
+    }
     {
         const Rescale r(ref, to, c);
         if constexpr (ENTROPY) xs = r.f * (xs + r.dx * s);
         s *= r.f;
     }
     // the owner's logits once more: those below the largest, and how many equal it
-    float equal = 0.f;
+    float equal = 0.f, again = 0.f;
     {
         if (tid == owner) s = s == s ? 0.f : s;
-        float again = 0.f;
-        auto below = [&](const u32x4_t piece) __attribute__((always_inline)) {
-            float v[P::N];
-            P::get(piece, v);
+        float v[P::N + 1];
+        P::get(own, v);
+        v[P::N] = tid == owner ? edge : -__builtin_inff();
 #pragma unroll
-            for (int k = 0; k < P::N; ++k) {
-                const float e = __builtin_amdgcn_exp2f((v[k] - to) * c);
-                again += v[k] < top ? e : 0.f;
-                equal += v[k] == top ? 1.f : 0.f;
-            }
-        };
-        if (batches > 1) {
-            for (int i = tid; i * NT + owner < pieces; i += NT) below(*reinterpret_cast<const u32x4_t *>(zp + (int64_t)(i * NT + owner) * P::N));
-        } else if (tid == owner && batches == 1) {            // still at hand
-#pragma unroll
-            for (int u = 0; u < PIECES; ++u) below(last[u]);
+        for (int k = 0; k <= P::N; ++k) {
+            const float e = __builtin_amdgcn_exp2f((v[k] - to) * c);
+            again += v[k] < top ? e : 0.f;
+            equal += v[k] == top ? 1.f : 0.f;
         }
-        if (tid == owner && edge_at >= 0) {
-            const float e = __builtin_amdgcn_exp2f((edge - to) * c);
-            again += edge < top ? e : 0.f;
-            equal += edge == top ? 1.f : 0.f;
-        }
-        s += again;
     }
-    s = wave_sum(s);
+    s = wave_sum(s + again);
     equal = wave_sum(equal);
     if constexpr (ENTROPY) xs = wave_sum(xs);
     if (lane == 0) {
         sums[0][wave] = s;
         sums[1][wave] = equal;
         sums[2][wave] = xs;
-    }
-    __shared__ uint32_t bound;
-    __shared__ int n_blocks, n_found;
-    if constexpr (TOP) {
-        if (wave == 0) {
-            uint32_t order[WAVES];
-#pragma unroll
-            for (int i = 0; i < WAVES; ++i) order[i] = order_of(thread_m[i * 64 + lane]);
-            const uint32_t l = bound_of<WAVES>(order, a.top_n);
-            if (lane == 0) {
-                bound = l;
-                n_blocks = n_found = 0;
-            }
-        }
     }
     __syncthreads();
     RowSums r;
@@ -357,66 +375,55 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
         r.rest = top == -__builtin_inff() ? others - 1.f : others + (same - 1.f);
     }
 
+    const float log_s = log1pf(r.rest);
+    if (tid == NT - 64) {                                     // (the last wavefront has the least to do below)
+        if (parts > 1) out.sums[row * parts + p] = r;
+        else finish_row(a, row, r, log_s, target, target_z);
+    }
     if constexpr (TOP) {
-        __shared__ uint64_t found[FOUND];
-        __shared__ uint16_t blocks[FOUND];
         const int n = a.top_n;
-        const float least = value_of(bound);
-        for (int i = tid; i < (batches + 1) * NT; i += NT)
-            // (blocks of nothing, the last ones and those of threads without a value of their own in the last row, are passed over)
-            if (block_max[i] >= least && (i >= batches * NT ? edge_at >= 0 : i / NT * PIECES * NT + tid < pieces)) {
-                const int at = atomicAdd(&n_blocks, 1);
-                if (at < FOUND) blocks[at] = (uint16_t)i;
-            }
-        __syncthreads();
         const int nb = n_blocks;
-        bool fits = r.rest == r.rest && nb <= FOUND;
-        if (fits)
-            for (int i = tid; i < nb * PIECES; i += NT) {
-                const int block = blocks[i / PIECES], u = i % PIECES, b = block / NT, t = block % NT;
-                float v[P::N];
-                int at;                                       // of v[0]
-                if (b == batches) {                           // a value outside whole pieces
-                    at = t < head ? t : t >= 32 && t - 32 < len - behind ? behind + t - 32 : -1;
-                    if (u > 0 || at < 0) continue;
-                    v[0] = widen(zs[at]);
+        const bool few = r.rest == r.rest && nb <= FOUND;
+        if (few)
+            for (int i0 = tid; i0 < nb * WORDS; i0 += 2 * NT) {
+                uint32_t word[2];                             // 4 bytes of a block each, both on their way
+                int at[2];
 #pragma unroll
-                    for (int k = 1; k < P::N; ++k) v[k] = __builtin_nanf("");
-                } else {
-                    const int piece = (b * PIECES + u) * NT + t;
-                    if (piece >= pieces) continue;
-                    P::get(*reinterpret_cast<const u32x4_t *>(zp + (int64_t)piece * P::N), v);
-                    at = head + piece * P::N;
+                for (int j = 0; j < 2; ++j) {
+                    const int i = i0 + j * NT, block = blocks[i / WORDS < nb ? i / WORDS : 0], u = i % WORDS / 4;
+                    const int piece = (block / NT * PIECES + u) * NT + block % NT;
+                    at[j] = -1;
+                    if (i >= nb * WORDS || piece >= pieces) continue;
+                    at[j] = v0 + head + piece * P::N + i % 4 * (P::N / 4);
+                    word[j] = *reinterpret_cast<const uint32_t *>(z + at[j]);
                 }
-                int reach = 0;
 #pragma unroll
-                for (int k = 0; k < P::N; ++k) reach += v[k] >= least;
-                if (reach == 0) continue;
-                int to = atomicAdd(&n_found, reach);
+                for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int k = 0; k < P::N; ++k)
-                    if (v[k] >= least) {
-                        if (to < FOUND) found[to] = rank_key(v[k], v0 + at + k);
-                        ++to;
+                    for (int k = 0; k < P::N / 4; ++k) {
+                        const float v = __uint_as_float(DT == REMOE_F32 ? word[j] : k == 0 ? word[j] << 16 : word[j] & 0xFFFF0000u);
+                        if (at[j] >= 0 && v >= least) {
+                            const int to = atomicAdd(&n_found, 1);
+                            if (to < FOUND) found[to] = rank_key(v, at[j] + k);
+                        }
                     }
             }
         __syncthreads();
         int nf = n_found;
-        fits = fits && nf <= FOUND;
-        if (!fits) {
+        if (!few || nf > FOUND) {
             __syncthreads();                                  // every thread has read n_found
-            const int quarter = (len + WAVES - 1) / WAVES;
-            const int lo = wave * quarter, hi = lo + quarter < len ? lo + quarter : len;
-            const uint64_t mine = sorted_list<DT>(zs, lo, hi, n);
-            // (ids of the part so far)
-            found[tid] = lane < n && mine ? mine - (uint64_t)v0 : 0;
+            SortedList list;
+            const int share = (pieces + WAVES - 1) / WAVES, p0 = wave * share;
+            offer_pieces<DT>(list, zp, v0 + head, p0, p0 + share < pieces ? p0 + share : pieces, n);
+            if (wave == 0) list.offer(edge_at >= 0 ? rank_key(edge, v0 + edge_at) : 0, n);
+            found[tid] = lane < n ? list.mine : 0;
             nf = NT;
             __syncthreads();
         }
         ranked<NT>(found, nf, n, [&](int rank, uint64_t key) {
             if (parts == 1) {
                 a.top_idx[row * n + rank] = key_id(key);
-                a.top_logprob[row * n + rank] = log_p(r, value_of((uint32_t)(key >> 32)), a.tau);
+                a.top_logprob[row * n + rank] = log_p(r, log_s, value_of((uint32_t)(key >> 32)), a.tau);
             } else {
                 out.keys[(row * parts + p) * n + rank] = key;
             }
@@ -424,19 +431,16 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
         if (parts > 1)                                        // a part shorter than n
             for (int j = len + tid; j < n; j += NT) out.keys[(row * parts + p) * n + j] = 0;
     }
-    if (parts > 1) {
-        if (tid == 0) out.sums[row * parts + p] = r;
-    } else {
-        finish_row<NT>(a, row, z, r, target, target_z, part);
-    }
+    if constexpr (TEACHER)
+        if (parts == 1) finish_teacher<NT>(a, row, z, r, part);
 }
 
 // The parts of a row, a lane each.
-constexpr int JOIN_THREADS = 256;
+constexpr int JOIN_THREADS = 256, JOIN_WAVES = JOIN_THREADS / 64;
 template <int DT> __global__ __launch_bounds__(JOIN_THREADS) void head_join_kernel(const HeadArgs a, int parts, PartOut in)
 {
     typedef typename LogitOf<DT>::type elem;
-    __shared__ double part[JOIN_THREADS / 64];
+    __shared__ double part[JOIN_WAVES];
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, n = a.top_n;
     const elem *z = static_cast<const elem *>(a.logits) + row * a.ld;
@@ -454,55 +458,76 @@ template <int DT> __global__ __launch_bounds__(JOIN_THREADS) void head_join_kern
     r.xsum = wave_sum(scale.f * (r.xsum + scale.dx * whole));
     r.rest = wave_sum(lane == owner ? r.rest : whole * scale.f);
     r.m = top;
+    const float log_s = log1pf(r.rest);
+    if (tid == JOIN_THREADS - 64) finish_row(a, row, r, log_s, target, target_z);
     if (n > 0) {
         constexpr int EACH = MAX_PARTS * MAX_N / JOIN_THREADS;
-        __shared__ uint64_t found[MAX_PARTS * MAX_N], thread_top[JOIN_THREADS], bound;
+        __shared__ uint64_t found[MAX_PARTS * MAX_N];
+        __shared__ uint32_t wave_bound[JOIN_WAVES];
         __shared__ int n_found;
         uint64_t key[EACH], most = 0;
+        // all parts' first keys, then their second, ...: a thread's first is its largest or close to it
+        int p = tid % parts, rank = tid / parts;
+        const int dp = JOIN_THREADS % parts, dr = JOIN_THREADS / parts;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            // all parts' first keys, then their second, ...: a thread's first is its largest or close to it
-            const int at = i * JOIN_THREADS + tid;
-            key[i] = at < parts * n ? in.keys[(row * parts + at % parts) * n + at / parts] : 0;
+            key[i] = rank < n ? in.keys[(row * parts + p) * n + rank] : 0;
+            rank += dr + (p + dp >= parts);
+            p += p + dp >= parts ? dp - parts : dp;
         }
 #pragma unroll
         for (int i = 0; i < EACH; ++i) most = key[i] > most ? key[i] : most;
-        thread_top[tid] = most;
+        const uint32_t reached = bound_of((uint32_t)(most >> 32), (n + JOIN_WAVES - 1) / JOIN_WAVES);
+        if (lane == 0) wave_bound[tid >> 6] = reached;
         if (tid == 0) n_found = 0;
         __syncthreads();
-        if (tid < 64) {
-            uint64_t value[JOIN_THREADS / 64];
+        uint32_t bound = wave_bound[0];
 #pragma unroll
-            for (int i = 0; i < JOIN_THREADS / 64; ++i) value[i] = thread_top[i * 64 + lane];
-            const uint64_t l = bound_of<JOIN_THREADS / 64>(value, n);
-            if (lane == 0) bound = l;
-        }
-        __syncthreads();
+        for (int w = 1; w < JOIN_WAVES; ++w) bound = min(bound, wave_bound[w]);
 #pragma unroll
         for (int i = 0; i < EACH; ++i)
-            if (key[i] && key[i] >= bound) found[atomicAdd(&n_found, 1)] = key[i];
+            if (key[i] && (uint32_t)(key[i] >> 32) >= bound) found[atomicAdd(&n_found, 1)] = key[i];
         __syncthreads();
         ranked<JOIN_THREADS>(found, n_found, n, [&](int rank, uint64_t k) {
             a.top_idx[row * n + rank] = key_id(k);
-            a.top_logprob[row * n + rank] = log_p(r, value_of((uint32_t)(k >> 32)), a.tau);
+            a.top_logprob[row * n + rank] = log_p(r, log_s, value_of((uint32_t)(k >> 32)), a.tau);
         });
     }
-    finish_row<JOIN_THREADS>(a, row, z, r, target, target_z, part);
+    if (a.teacher_idx) finish_teacher<JOIN_THREADS>(a, row, z, r, part);
 }
 
 // How rows are dealt out: threads of a workgroup, parts of a row, logits of a part.
 struct Cut { int threads, parts, len; };
-Cut cut_rows(int dtype, int V, int64_t T)
+
+// a bit of a mask for every batch of a thread, a thread for every piece of the owner's, no more LDS than lets four share a compute unit
+int64_t longest_part(int threads, int per)
 {
-    const int per = dtype == REMOE_BF16 ? 8 : 4, threads = HS_NT, unit = threads * per;
-    const int64_t least = ceil_div(V, MAX_PART);
-    int64_t parts = T > 0 ? ceil_div(HS_WORKGROUPS, T) : MAX_PARTS;
-    const int64_t most = ceil_div(V, HS_MIN_UNITS * unit);
-    if (parts > most) parts = most;
-    if (parts > MAX_PARTS) parts = MAX_PARTS;
-    if (parts < least) parts = least;
-    int64_t len = align_up(ceil_div(V, parts), unit);
-    if (len > MAX_PART) len = MAX_PART;
+    const int64_t bits = (int64_t)threads * BATCH * MAX_BATCHES, owners = (int64_t)threads * threads * per;
+    return bits < owners ? (bits < MAX_PART ? bits : MAX_PART) : (owners < MAX_PART ? owners : MAX_PART);
+}
+
+// A row is one workgroup's unless there are few and long ones: a second launch costs what 64 K logits take (T rows, one part / four
+// of 38 K: 8 rows of 151,936 14.8 / 10.7 us, 64 15.8 / 11.4, 256 18.9 / 21.9, 8 of 32,000 6.8 / 10.9).
+constexpr int CUT_FROM = 65536, CUT_LEN = 32768, CUT_WORKGROUPS = 512;
+// A wavefront a row where rows are short and many (no barrier waits for another; 8192 rows of 2048: 64 / 256 threads 16 / 30 us; of
+// 8192 36 / 35, with 20 alternatives 51 / 57); not for more alternatives than half its lanes, whose bound is too low (1024 rows of 2048,
+// 64 alternatives: 102 / 14).  Two workgroups' threads for few long rows (256 of 151,936: 256 / 512 threads 21.1 / 18.9 us; 1024
+// 71 / 71; 64 of 32,000 6.6 / 7.3).
+constexpr int SHORT_ROW = 8192, MANY_ROWS = 1024, FEW_ROWS = 256;
+
+// entries: alternatives or a teacher's tokens
+Cut cut_rows(int dtype, int V, int64_t T, int top_n, int K)
+{
+    const int per = dtype == REMOE_BF16 ? 8 : 4;
+    int threads = 256;
+    if (V >= CUT_FROM && T <= FEW_ROWS) threads = 512;
+    else if (V <= SHORT_ROW && T >= MANY_ROWS && top_n <= 32) threads = 64;
+    while (threads > 64 && V < threads * per) threads >>= 1;  // every lane has a piece
+    while (threads < K) threads <<= 1;                        // and a teacher's every entry a thread
+    int64_t parts = ceil_div(V, longest_part(threads, per));
+    const int64_t more = ceil_div(V, CUT_LEN);
+    if (V >= CUT_FROM && T * more <= CUT_WORKGROUPS && parts < more) parts = more < MAX_PARTS ? more : MAX_PARTS;
+    const int64_t len = align_up(ceil_div(V, parts), threads * per);
     return {threads, (int)ceil_div(V, len), (int)len};
 }
 
@@ -511,11 +536,13 @@ template <int NT> remoe_status launch_scan(const HeadArgs &a, const Cut &cut, co
     const bool bf16 = a.dtype == REMOE_BF16, entropy = a.entropy != nullptr, top = a.top_n > 0;
     auto kernel = [&]() {
         if (bf16) {
-            if (top) return entropy ? head_scan_kernel<NT, REMOE_BF16, true, true> : head_scan_kernel<NT, REMOE_BF16, false, true>;
-            return entropy ? head_scan_kernel<NT, REMOE_BF16, true, false> : head_scan_kernel<NT, REMOE_BF16, false, false>;
+            if (a.teacher_idx) return head_scan_kernel<NT, REMOE_BF16, false, false, true>;
+            if (top) return entropy ? head_scan_kernel<NT, REMOE_BF16, true, true, false> : head_scan_kernel<NT, REMOE_BF16, false, true, false>;
+            return entropy ? head_scan_kernel<NT, REMOE_BF16, true, false, false> : head_scan_kernel<NT, REMOE_BF16, false, false, false>;
         }
-        if (top) return entropy ? head_scan_kernel<NT, REMOE_F32, true, true> : head_scan_kernel<NT, REMOE_F32, false, true>;
-        return entropy ? head_scan_kernel<NT, REMOE_F32, true, false> : head_scan_kernel<NT, REMOE_F32, false, false>;
+        if (a.teacher_idx) return head_scan_kernel<NT, REMOE_F32, false, false, true>;
+        if (top) return entropy ? head_scan_kernel<NT, REMOE_F32, true, true, false> : head_scan_kernel<NT, REMOE_F32, false, true, false>;
+        return entropy ? head_scan_kernel<NT, REMOE_F32, true, false, false> : head_scan_kernel<NT, REMOE_F32, false, false, false>;
     }();
     const int64_t longest = cut.len < a.V ? cut.len : a.V;
     const size_t lds = top ? sizeof(float) * NT * (ceil_div(longest, NT * BATCH) + 1) : 0;
@@ -525,27 +552,29 @@ template <int NT> remoe_status launch_scan(const HeadArgs &a, const Cut &cut, co
 
 }  // namespace
 
-// Never less for more tokens: T rows have at most T times the parts of one, and no more than HS_WORKGROUPS + T <= 2 HS_WORKGROUPS
-// unless MAX_PART cuts every row (a row that is not cut leaves nothing here).
+// Never less for more tokens: so many rows as are cut because they are few, or all of them where a row is longer than a part.
+// (The parts of a row depend neither on the alternatives nor on the teacher's list, which only matter to shorter rows.)
 size_t head_workspace_bytes(int dtype, int V, int64_t T, int top_n)
 {
-    const Cut one = cut_rows(dtype, V, 1);
-    const int64_t least = ceil_div(V, MAX_PART);
-    int64_t slots = T * one.parts;
-    const int64_t enough = 2 * HS_WORKGROUPS + (least > 1 ? T * least : 0);
-    if (slots > enough) slots = enough;
+    const int64_t more = ceil_div(V, CUT_LEN), most = CUT_WORKGROUPS / (more < CUT_WORKGROUPS ? more : CUT_WORKGROUPS);
+    const int64_t always = ceil_div(V, MAX_PART);
+    int64_t slots = V >= CUT_FROM ? (T < most ? T : most) * cut_rows(dtype, V, 1, 0, 0).parts : 0;
+    if (always > 1 && slots < T * always) slots = T * always;
     return align_up(sizeof(RowSums) * (size_t)slots, 256) + align_up(sizeof(uint64_t) * (size_t)slots * top_n, 256) + 256;
 }
 
 remoe_status launch_head_forward(const HeadArgs &a, hipStream_t stream)
 {
-    const Cut cut = cut_rows(a.dtype, a.V, a.T);
+    const Cut cut = cut_rows(a.dtype, a.V, a.T, a.top_n, a.K);
     PartOut out{};
     if (cut.parts > 1) {
         out.sums = static_cast<RowSums *>(a.workspace);
         out.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(a.workspace) + align_up(sizeof(RowSums) * (size_t)(a.T * cut.parts), 256));
     }
-    const remoe_status st = launch_scan<HS_NT>(a, cut, out, stream);
+    const remoe_status st = cut.threads == 64    ? launch_scan<64>(a, cut, out, stream)
+                            : cut.threads == 128 ? launch_scan<128>(a, cut, out, stream)
+                            : cut.threads == 256 ? launch_scan<256>(a, cut, out, stream)
+                                                 : launch_scan<512>(a, cut, out, stream);
     if (st != REMOE_OK || cut.parts == 1) return st;
     hipLaunchKernelGGL(a.dtype == REMOE_BF16 ? head_join_kernel<REMOE_BF16> : head_join_kernel<REMOE_F32>, dim3((unsigned)a.T), dim3(JOIN_THREADS), 0,
                        stream, a, cut.parts, out);

@@ -533,3 +533,36 @@ def test_the_binding_refuses_wrong_tensors():
     with pytest.raises(remoe.RemoeError, match="teacher_idx"):
         remoe.remoe_distill_forward(desc, z, i32, torch.zeros(4, 1, device=DEV), None, g, None, ws)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V,n", [(5, 3), (70, 64), (600, 20), (1000, 64), (1500, 33), (2048, 32), (2100, 64), (5000, 5), (8192, 20), (8193, 64)])
+def test_many_short_rows(V, n, dtype):
+    """A wavefront a row, or two: rows of every kind, those that leave fewer tokens than are asked for among them."""
+    T = 1030
+    print(f"many short rows V={V} n={n} {dtype}", flush=True)
+    z = rows(V + n, [KINDS[i % len(KINDS)] for i in range(T)], V, dtype, V + 1)
+    tgt = _targets(n, z)
+    _check_logprobs(_logprobs(_to_device(z, V + 1, 1), 0.7, tgt, n), z, 0.7, tgt, n)
+    if n != 33:
+        return
+    for K in (64, 65, 200):
+        _check_distill(z[:, :V].contiguous(), 1.0, K, False)
+
+
+@pytest.mark.parametrize("T,V,n", [(3, 151936, 20), (130, 70001, 64), (2, 300001, 64)])
+def test_long_rows_with_fewer_tokens_than_asked_for(T, V, n):
+    print(f"long masked rows T={T} V={V} n={n}", flush=True)
+    kinds = [("one", "empty", "all_lowest", "equal", "nan", "inf", "zeros")[t % 7] for t in range(T)]
+    z = rows(V, kinds, V, BF16)
+    z[0, torch.randperm(V, generator=torch.Generator().manual_seed(1))[:n // 2]] = 1.5       # a mask that leaves n / 2 of one value
+    tgt = _targets(V, z)
+    _check_logprobs(_logprobs(_to_device(z), 1.0, tgt, n), z, 1.0, tgt, n)
+
+
+@pytest.mark.parametrize("T,V,dtype", [(200, 70001, BF16), (300, 70001, BF16), (100, 65536, F32), (102, 151936, BF16), (103, 151936, BF16)])
+def test_where_rows_are_dealt_out_otherwise(T, V, dtype):
+    print(f"threads and parts T={T} V={V} {dtype}", flush=True)
+    z = rows(T, [("plain", "masked", "ties", "few")[t % 4] for t in range(T)], V, dtype)
+    tgt = _targets(V, z)
+    _check_logprobs(_logprobs(_to_device(z), 1.0, tgt, 20), z, 1.0, tgt, 20)
