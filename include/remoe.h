@@ -440,7 +440,7 @@ remoe_status remoe_gate_grad(const float *dlogits, const void *x, int32_t x_dtyp
  *   fixed order, results repeat bit for bit.  -inf masks a token: probability 0, gradient 0.  A row of nothing but
  *   -inf has stats (-inf, -1), ln p = -inf for every token, entropy 0 and gradient 0.  A row that holds NaN or +inf
  *   has rest = NaN (its max is unspecified), and its log probabilities, entropy, losses and gradients are NaN.
- *   vocab 1..2^24, temperature positive, finite and not below 2^-20; n_tokens 0..2^22 (0 launches nothing).
+ *   vocab 1..2^24, temperature 2^-20..2^20, ld up to 2^32, n_tokens 0..2^22 (0 launches nothing).
  */
 typedef struct {
     int32_t vocab;         /* V                                                                      */
@@ -479,7 +479,7 @@ remoe_status remoe_token_logprobs(const remoe_head_desc *desc, const void *logit
  *   d_logprob       [T] fp32, or NULL together with targets;  entropy, d_entropy [T] fp32, or both NULL; one pair is given
  *   accumulate      0: dlogits is written; 1: added to (in fp32, rounded once)
  *   dlogits         [T, V] of desc->dtype with row stride ld_d >= vocab.  With accumulate 0 it may be `logits` itself
- *                   (same pointer and row stride); any other overlap of the two is refused
+ *                   (same pointer and row stride); any other overlap of the two address ranges is refused
  */
 remoe_status remoe_token_logprobs_backward(const remoe_head_desc *desc, const void *logits, int64_t n_tokens, int64_t ld,
                                            const float *stats, const int32_t *targets, const float *d_logprob,

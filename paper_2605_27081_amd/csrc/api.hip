@@ -721,8 +721,8 @@ static remoe_status validate_head(const remoe_head_desc *d, int64_t T)
     if (d->vocab < 1 || d->vocab > MAX_VOCAB) return fail(REMOE_E_INVALID_ARG, "vocab %d outside 1..%d", d->vocab, MAX_VOCAB);
     if (d->dtype != REMOE_F32 && d->dtype != REMOE_BF16)
         return fail(REMOE_E_INVALID_ARG, "dtype %d is neither REMOE_F32 nor REMOE_BF16", d->dtype);
-    if (!(d->temperature >= 0x1p-20f) || d->temperature > 3.0e38f)
-        return fail(REMOE_E_INVALID_ARG, "temperature must be finite and at least 2^-20");
+    if (!(d->temperature >= 0x1p-20f && d->temperature <= 0x1p20f))
+        return fail(REMOE_E_INVALID_ARG, "temperature %g outside 2^-20..2^20", (double)d->temperature);
     if (T < 0 || T > MAX_TOKENS) return fail(REMOE_E_INVALID_ARG, "n_tokens %lld outside 0..%lld", (long long)T, (long long)MAX_TOKENS);
     return REMOE_OK;
 }

@@ -22,7 +22,7 @@ namespace remoe {
 
 namespace {
 
-constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
+constexpr float LN2 = 0.693147180559945309417f;
 constexpr float LOWEST = -3.402823466e38f;
 constexpr int BATCH = 32;                               // logits of a thread that are taken together
 constexpr int MAX_BATCHES = 32;                         // of a thread: bits of a mask
@@ -35,11 +35,11 @@ constexpr int FOUND = 512;                              // logits that may reach
 // (x = log2 e d)
 struct RowSums { float m, rest, xsum; };
 
-// ln p of a logit; log_s = log1p(rest).  (Code that a row passes once is kept short throughout: few rows find none of it in the
+// ln p of a logit; log_s = log1p(rest).  In fp64: the difference of two fp32 numbers may be none.  (Code that a row passes once is kept short throughout: few rows find none of it in the
 // instruction cache, and 64 bytes of it cost 100 cycles then.)
 __device__ __forceinline__ float log_p(const RowSums &r, float log_s, float z, float tau)
 {
-    return r.rest == -1.f ? -__builtin_inff() : (z - r.m) / tau - log_s;      // (-1: nothing but -inf)
+    return r.rest == -1.f ? -__builtin_inff() : (float)(((double)z - (double)r.m) / (double)tau - (double)log_s);      // (-1: nothing but -inf)
 }
 
 // Order of the alternatives: larger logits first, NaN above all, the lower id first among equals.
@@ -55,11 +55,24 @@ __device__ __forceinline__ float value_of(uint32_t order)
 __device__ __forceinline__ uint64_t rank_key(float z, int id) { return (uint64_t)order_of(z) << 32 | (0xFFFFFFFFu - (uint32_t)id); }
 __device__ __forceinline__ int key_id(uint64_t key) { return (int)(0xFFFFFFFFu - (uint32_t)key); }
 
+// x = log2 e d from a difference of logits.  log2 e / tau is not an fp32 number: what is cut off it would make every exponential
+// wrong in the same direction, by up to 2^-23 |d|, so it is multiplied in as well.
+struct Scale {
+    float c, low;                                             // c rounded towards 0; low > 0, so that -inf stays -inf
+    __device__ __forceinline__ explicit Scale(float tau)
+    {
+        const double all = 1.4426950408889634074 / (double)tau;
+        c = __double2float_rz(all);
+        low = fmaxf((float)(all - (double)c), 1e-30f);
+    }
+    __device__ __forceinline__ float x(float d) const { return fmaf(d, low, d * c); }
+};
+
 // The scale from sums relative to `from` to sums relative to `to`, and the shift of x.  2^-512 is 0, and the floor keeps
 // -inf out of products with 0.
 struct Rescale {
     float dx, f;
-    __device__ __forceinline__ Rescale(float from, float to, float c) : dx(fmaxf((from - to) * c, -512.f)), f(__builtin_amdgcn_exp2f(dx)) {}
+    __device__ __forceinline__ Rescale(float from, float to, const Scale &c) : dx(fmaxf(c.x(from - to), -512.f)), f(__builtin_amdgcn_exp2f(dx)) {}
 };
 
 // The outputs of a row that one thread writes, from its sums.  target, target_z: its token and that one's logit.
@@ -216,7 +229,7 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
 {
     typedef typename LogitOf<DT>::type elem;
     typedef Piece<DT> P;
-    constexpr int PIECES = BATCH / P::N, WORDS = PIECES * 4, WAVES = NT / 64;
+    constexpr int PIECES = BATCH / P::N, WAVES = NT / 64;
     extern __shared__ float block_max[];                      // [batches + 1, threads]: the maxima of every 32 logits
     __shared__ double part[TEACHER ? WAVES : 1];
     __shared__ float wave_m[WAVES], sums[3][WAVES];
@@ -236,7 +249,7 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
     const int pieces = (len - head) / P::N, behind = head + pieces * P::N;
     const elem *zp = zs + head;
     const int batches = (pieces + PIECES * NT - 1) / (PIECES * NT);
-    const float c = LOG2E / a.tau;
+    const Scale c(a.tau);
 
     u32x4_t next[PIECES];
     auto request = [&](int batch) __attribute__((always_inline)) {
@@ -257,7 +270,7 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
 
     // m: largest so far; s, xs: sums relative to ref, which is m, or the lowest number there is
     float m = edge, ref = fmaxf(edge, LOWEST), s = 0.f, xs = 0.f;
-    if (edge_at >= 0) s = __builtin_amdgcn_exp2f((edge - ref) * c);
+    if (edge_at >= 0) s = __builtin_amdgcn_exp2f(c.x(edge - ref));
     if constexpr (TOP) block_max[batches * NT + tid] = edge;
     for (int b = 0; b < batches; ++b) {
         float v[BATCH];
@@ -277,7 +290,7 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
         float s4[4] = {0.f, 0.f, 0.f, 0.f}, x4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const float x = (v[i] - to) * c, e = __builtin_amdgcn_exp2f(x);
+            const float x = c.x(v[i] - to), e = __builtin_amdgcn_exp2f(x);
             s4[i & 3] += e;
             if constexpr (ENTROPY) x4[i & 3] = fmaf(fmaxf(x, -512.f), e, x4[i & 3]);
         }
@@ -347,7 +360,7 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
         v[P::N] = tid == owner ? edge : -__builtin_inff();
 #pragma unroll
         for (int k = 0; k <= P::N; ++k) {
-            const float e = __builtin_amdgcn_exp2f((v[k] - to) * c);
+            const float e = __builtin_amdgcn_exp2f(c.x(v[k] - to));
             again += v[k] < top ? e : 0.f;
             equal += v[k] == top ? 1.f : 0.f;
         }
@@ -385,28 +398,22 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
         const int nb = n_blocks;
         const bool few = r.rest == r.rest && nb <= FOUND;
         if (few)
-            for (int i0 = tid; i0 < nb * WORDS; i0 += 2 * NT) {
-                uint32_t word[2];                             // 4 bytes of a block each, both on their way
-                int at[2];
+            for (int i = tid; i < nb * PIECES; i += NT) {
+                const int block = blocks[i / PIECES], piece = (block / NT * PIECES + i % PIECES) * NT + block % NT;
+                if (piece >= pieces) continue;
+                float v[P::N];
+                P::get(*reinterpret_cast<const u32x4_t *>(zp + (int64_t)piece * P::N), v);
+                uint32_t reach = 0;
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int i = i0 + j * NT, block = blocks[i / WORDS < nb ? i / WORDS : 0], u = i % WORDS / 4;
-                    const int piece = (block / NT * PIECES + u) * NT + block % NT;
-                    at[j] = -1;
-                    if (i >= nb * WORDS || piece >= pieces) continue;
-                    at[j] = v0 + head + piece * P::N + i % 4 * (P::N / 4);
-                    word[j] = *reinterpret_cast<const uint32_t *>(z + at[j]);
+                for (int k = 0; k < P::N; ++k) reach |= v[k] >= least ? 1u << k : 0u;
+                while (reach) {
+                    const int k = __ffs(reach) - 1, to = atomicAdd(&n_found, 1);
+                    reach &= reach - 1;
+                    float vk = v[0];
+#pragma unroll
+                    for (int j = 1; j < P::N; ++j) vk = k == j ? v[j] : vk;
+                    if (to < FOUND) found[to] = rank_key(vk, v0 + head + piece * P::N + k);
                 }
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int k = 0; k < P::N / 4; ++k) {
-                        const float v = __uint_as_float(DT == REMOE_F32 ? word[j] : k == 0 ? word[j] << 16 : word[j] & 0xFFFF0000u);
-                        if (at[j] >= 0 && v >= least) {
-                            const int to = atomicAdd(&n_found, 1);
-                            if (to < FOUND) found[to] = rank_key(v, at[j] + k);
-                        }
-                    }
             }
         __syncthreads();
         int nf = n_found;
@@ -444,7 +451,7 @@ template <int DT> __global__ __launch_bounds__(JOIN_THREADS) void head_join_kern
     const int64_t row = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, n = a.top_n;
     const elem *z = static_cast<const elem *>(a.logits) + row * a.ld;
-    const float c = LOG2E / a.tau;
+    const Scale c(a.tau);
     int target = -1;
     float target_z = 0.f;
     request_target(a, row, z, target, target_z);
@@ -546,6 +553,8 @@ template <int NT> remoe_status launch_scan(const HeadArgs &a, const Cut &cut, co
     }();
     const int64_t longest = cut.len < a.V ? cut.len : a.V;
     const size_t lds = top ? sizeof(float) * NT * (ceil_div(longest, NT * BATCH) + 1) : 0;
+    if (a.T * cut.parts * NT > 0xFFFFFFFFll)
+        return fail(REMOE_E_UNSUPPORTED, "%lld rows in %d parts are more than one launch can count", (long long)a.T, cut.parts);
     hipLaunchKernelGGL(kernel, dim3((unsigned)(a.T * cut.parts)), dim3(NT), lds, stream, a, cut.parts, cut.len, out);
     return check_hip(hipGetLastError(), "head_scan_kernel launch");
 }

@@ -5,21 +5,19 @@
 //
 // A pass over the row writes the terms that every token has; the tokens that are named (the target, the teacher's) are taken
 // from their logits in fp64 and written over it: their differences cancel where the model agrees (1 - p_v, M p_v - q_v).
-// A workgroup has a stretch of a row's 16-byte pieces, cut where dlogits is aligned, and all of its named tokens.
+// A workgroup has a stretch of a row's 16-byte pieces, cut where dlogits is aligned, and the named tokens among its values.  The
+// first pieces are asked for before the row's terms are known, the next ones before the present ones are used, and the stores
+// go past the caches (non-temporal: 4096 rows of 151,936 with a teacher's list 586 -> 545 us).
+//
+// Bound by HBM: every logit is read and every gradient written once.  8192 rows of 151,936 bf16 logits 970 us = 5.1 TB/s (a plain
+// copy of 4 GiB 4.7), with a list of 128 for 4096 rows 508 us = 4.9 TB/s; 1021 rows of 50,257 36 us.
 #include "head_rows.h"
 
 namespace remoe {
 
 namespace {
 
-#ifndef HG_PIECES
-#define HG_PIECES 2
-#endif
-#ifndef HG_WORKGROUPS
-#define HG_WORKGROUPS 8192
-#endif
-constexpr int NT = 256;
-constexpr int PIECES = HG_PIECES;      // 16-byte pieces of a thread that are on their way together
+constexpr int PIECES = 2;              // 16-byte pieces of a thread that are on their way together
 
 // dz = e * (k0 + k1 x) with x = log2 e, away from the named tokens
 struct RowTerms { float m, c, c_low, k0, k1; };
@@ -38,7 +36,7 @@ template <bool FINE> __device__ __forceinline__ float term(const RowTerms &t, fl
 __device__ __forceinline__ void put_one(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put_one(bf16_t *p, float v) { *p = (bf16_t)(pack_bf16x2(v, 0.f) & 0xFFFFu); }
 
-template <int DT, bool TEACHER, bool ADD>
+template <int NT, int DT, bool TEACHER, bool ADD>
 __global__ __launch_bounds__(NT) void head_grad_kernel(const HeadGradArgs a, int segs, int seg_pieces)
 {
     typedef typename LogitOf<DT>::type elem;
@@ -144,7 +142,7 @@ __global__ __launch_bounds__(NT) void head_grad_kernel(const HeadGradArgs a, int
         const int behind = head + pieces * P::N;
         int v = -1;
         if (seg == 0 && tid < head) v = tid;
-        if (seg == segs - 1 && tid >= 64 && tid - 64 < V - behind) v = behind + tid - 64;
+        if (seg == segs - 1 && tid >= 32 && tid - 32 < V - behind) v = behind + tid - 32;
         if (v >= 0) put_one(dz + v, term<FINE>(t, widen(z[v])) + (ADD ? widen(dz[v]) : 0.f));
     }
     for (int p = p0 + tid; p < p1; p += PIECES * NT) {
@@ -172,27 +170,41 @@ __global__ __launch_bounds__(NT) void head_grad_kernel(const HeadGradArgs a, int
 
 }  // namespace
 
-remoe_status launch_head_backward(const HeadGradArgs &a, hipStream_t stream)
+namespace {
+
+template <int NT> remoe_status launch_grad(const HeadGradArgs &a, int64_t segs, int seg_pieces, hipStream_t stream)
 {
-    const int per = a.dtype == REMOE_BF16 ? 8 : 4;
-    const int64_t pieces = ceil_div(a.V, per);
-    int64_t segs = ceil_div(HG_WORKGROUPS, a.T);
-    const int64_t most = ceil_div(pieces, NT);
-    if (segs > most) segs = most;
-    const int seg_pieces = (int)ceil_div(pieces, segs);
-    segs = ceil_div(pieces, seg_pieces);
     auto kernel = [&]() {
         const bool bf16 = a.dtype == REMOE_BF16;
         if (a.teacher_idx) {
-            if (a.accumulate) return bf16 ? head_grad_kernel<REMOE_BF16, true, true> : head_grad_kernel<REMOE_F32, true, true>;
-            return bf16 ? head_grad_kernel<REMOE_BF16, true, false> : head_grad_kernel<REMOE_F32, true, false>;
+            if (a.accumulate) return bf16 ? head_grad_kernel<NT, REMOE_BF16, true, true> : head_grad_kernel<NT, REMOE_F32, true, true>;
+            return bf16 ? head_grad_kernel<NT, REMOE_BF16, true, false> : head_grad_kernel<NT, REMOE_F32, true, false>;
         }
-        if (a.accumulate) return bf16 ? head_grad_kernel<REMOE_BF16, false, true> : head_grad_kernel<REMOE_F32, false, true>;
-        return bf16 ? head_grad_kernel<REMOE_BF16, false, false> : head_grad_kernel<REMOE_F32, false, false>;
+        if (a.accumulate) return bf16 ? head_grad_kernel<NT, REMOE_BF16, false, true> : head_grad_kernel<NT, REMOE_F32, false, true>;
+        return bf16 ? head_grad_kernel<NT, REMOE_BF16, false, false> : head_grad_kernel<NT, REMOE_F32, false, false>;
     }();
-    const dim3 grid((unsigned)(a.T * segs)), block(NT);
-    hipLaunchKernelGGL(kernel, grid, block, 0, stream, a, (int)segs, seg_pieces);
-    return check_hip(hipGetLastError(), "head gradient kernel launch");
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(a.T * segs)), dim3(NT), 0, stream, a, (int)segs, seg_pieces);
+    return check_hip(hipGetLastError(), "head_grad_kernel launch");
+}
+
+}  // namespace
+
+// Workgroups of 256 threads, enough of them to even out the compute units, each with at least 2 pieces a thread, or 4 where a
+// teacher's list is taken first (1024 rows of 8192: 1 / 2 pieces 9.9 / 8.1 us; 1024 of 32,000, 64 listed tokens: 2 / 4 pieces
+// 37.9 / 31.7; 333 of 102,400 fp32: 4096 / 8192 workgroups 60 / 53).  A wavefront a row where many rows are short: its sums over the
+// list wait for no other (8192 rows of 2048, 64 listed tokens: 256 / 64 threads 38.6 / 26.1 us; of 8192 66.5 / 71.2).
+constexpr int WORKGROUPS = 8192, SHORT_PIECES = 512, MANY_ROWS = 1024;
+
+remoe_status launch_head_backward(const HeadGradArgs &a, hipStream_t stream)
+{
+    const int64_t pieces = ceil_div(a.V, a.dtype == REMOE_BF16 ? 8 : 4);
+    const int threads = pieces <= SHORT_PIECES && a.T >= MANY_ROWS && a.K <= 64 ? 64 : 256;
+    const int64_t most = ceil_div(pieces, threads * (a.teacher_idx ? 4 : 2));
+    int64_t segs = ceil_div(WORKGROUPS, a.T);
+    if (segs > most) segs = most;
+    const int seg_pieces = (int)ceil_div(pieces, segs);
+    segs = ceil_div(pieces, seg_pieces);
+    return threads == 64 ? launch_grad<64>(a, segs, seg_pieces, stream) : launch_grad<256>(a, segs, seg_pieces, stream);
 }
 
 }  // namespace remoe

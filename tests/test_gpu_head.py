@@ -566,3 +566,37 @@ def test_where_rows_are_dealt_out_otherwise(T, V, dtype):
     z = rows(T, [("plain", "masked", "ties", "few")[t % 4] for t in range(T)], V, dtype)
     tgt = _targets(V, z)
     _check_logprobs(_logprobs(_to_device(z), 1.0, tgt, 20), z, 1.0, tgt, 20)
+
+
+@pytest.mark.parametrize("tau", [2.0 ** -20, 1e-3, 1e3, 2.0 ** 20])
+def test_extreme_temperatures(tau):
+    z = rows(71, KINDS, 3000, F32)
+    z = z.clamp(-3e5, 3e5) if tau < 1 else z               # (z - m) / tau within fp32
+    tgt = _targets(3, z)
+    _check_logprobs(_logprobs(_to_device(z), tau, tgt, 9), z, tau, tgt, 9)
+    g = torch.ones(len(KINDS))
+    _logprob_gradient(z, tau, tgt, g, g)
+
+
+def test_no_rows():
+    desc = _desc(100, BF16, 1.0)
+    z = torch.empty(0, 100, dtype=BF16, device=DEV)
+    ws = _workspace(desc, 0)[0]
+    i32 = torch.empty(0, dtype=torch.int32, device=DEV)
+    remoe.remoe_token_logprobs(desc, z, i32, _out(0), None, None, None, _out(0, 2), ws)
+    remoe.remoe_token_logprobs_backward(desc, z, _out(0, 2), i32, _out(0), None, None, z)
+    remoe.remoe_distill_forward(desc, z, i32.view(0, 1), _out(0, 1), None, _out(0), None, ws)
+    remoe.remoe_distill_backward(desc, z, _out(0, 2), i32.view(0, 1), _out(0, 1), None, _out(0), z)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("V", [5, 600, 2048, 4097])
+def test_gradients_of_many_short_rows(V):
+    T = 1030
+    print(f"gradients of many short rows V={V}", flush=True)
+    z = rows(V + 5, [KINDS[i % len(KINDS)] for i in range(T)], V, BF16)
+    d = torch.randn(T, generator=torch.Generator().manual_seed(V))
+    _logprob_gradient(z, 1.0, _targets(V, z), d, d)
+    for K, accumulate in ((1, False), (64, True), (65, False)):
+        idx, tl, lse = _teacher(V + K, z, K)
+        _distill_gradient(z, 1.0, idx, tl, lse if K == 64 else None, d, accumulate=accumulate)

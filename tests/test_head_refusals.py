@@ -44,7 +44,8 @@ CALLS = (_logprobs, _logprobs_backward, _distill, _distill_backward)
 @pytest.mark.parametrize("call", CALLS)
 @pytest.mark.parametrize("desc,word", [((0, 1, 1.0), "vocab"), ((-5, 1, 1.0), "vocab"), (((1 << 24) + 1, 1, 1.0), "vocab"), ((100, 2, 1.0), "dtype"),
                                        ((100, 1, 0.0), "temperature"), ((100, 1, -1.0), "temperature"), ((100, 1, float("nan")), "temperature"),
-                                       ((100, 1, float("inf")), "temperature"), ((100, 1, 1e-8), "temperature")])
+                                       ((100, 1, float("inf")), "temperature"), ((100, 1, 1e-8), "temperature"),
+                                       ((100, 1, 1.1e6), "temperature")])
 def test_descriptors(lib, call, desc, word):
     assert call(lib, desc=_desc(*desc)) == -1 and word in remoe.remoe_last_error()
     assert lib.remoe_head_workspace_bytes(_desc(*desc), 4, 0) == 0 and word in remoe.remoe_last_error()
@@ -127,3 +128,10 @@ def test_the_binding_refuses_host_tensors(lib):
     z = torch.zeros(2, 100, dtype=torch.bfloat16)
     with pytest.raises(remoe.RemoeError, match="device"):
         remoe.remoe_token_logprobs(remoe.HeadDesc(100, 1, 1.0), z, None, None, None, None, None, None, z)
+
+
+def test_more_rows_than_a_launch_counts(lib):
+    # 2^22 rows that are each cut into 64 parts: refused in front of the launch, whatever the addresses
+    d = _desc(1 << 24)
+    for call, kw in ((_logprobs, {}), (_distill, {})):
+        assert call(lib, desc=d, T=1 << 22, ld=1 << 24, **kw) == -2 and "launch" in remoe.remoe_last_error()
