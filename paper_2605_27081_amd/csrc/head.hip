@@ -4,17 +4,23 @@
 //   S = sum_v exp(d_v) = 1 + rest,  ln p_v = d_v - log1p(rest),  H = log1p(rest) - sum_v d_v exp(d_v) / S
 //   loss = sum_j q_j (ln q_j - ln p_id(j))
 //
-// head_scan_kernel reads a row, or a part of one, once: 16-byte pieces dealt out to 256 threads, each of which keeps the
-// largest logit it has seen and the sums of e^d and d e^d relative to it, 32 logits at a time.  rest leaves out the largest
-// logit's own 1, which a running sum cannot take back: the thread that has the largest logit has its pieces read once more (a
-// piece per thread of the workgroup).
+// head_scan_kernel reads a row, or a part of one, once: 16-byte pieces dealt out to the threads of a workgroup, each of which keeps
+// the largest logit it has seen and the sums of e^d and d e^d relative to it, 32 logits at a time, while the next 32 are on their
+// way.  rest leaves out the largest logit's own 1, which a running sum cannot take back: the thread that has the largest logit has
+// its pieces read once more, a piece by every thread of the workgroup.
 //
 // Alternatives: every wavefront has a bound that n / wavefronts of its lanes' maxima reach, so n logits of the row reach the
 // least of the bounds, and not many more do.  The maxima of every 32 logits are kept in LDS; those that reach it have their pieces
-// read again, and the logits found are ranked by counting the larger ones.  Where too many reach it (ties by the thousand: a mask that leaves fewer than n tokens), or
-// the row holds NaN, every wavefront keeps a sorted list, an entry per lane, over a quarter of the row.
+// read again, and the logits found are ranked by counting the larger ones.  Where too many reach it (ties by the thousand, as under
+// a mask that leaves fewer than n tokens), or the row holds NaN, every wavefront keeps a sorted list, an entry per lane, over its
+// share of the row.
 //
-// Few rows are cut into parts; head_join_kernel puts the parts together.
+// Long rows that are few are cut into parts; head_join_kernel puts the parts together.
+//
+// Bound by HBM for many rows: 8192 rows of 151,936 bf16 logits with entropy 434 us = 5.7 TB/s (8192 of 65,536 fp32: 6.1), where the
+// vector instructions (11.5 issue slots a bf16 logit, 4 of them the exponential) fill about nine tenths of the time; by those for less
+// than two rows a compute unit (333 rows of 102,400: 17 us); by latency for few (one row with 20 alternatives 9 + 6 us of kernels).  An
+// element at a time in three passes took 2530 us, 257 and 1767.
 #include "head_rows.h"
 #include "topk.h"
 
@@ -35,8 +41,8 @@ constexpr int FOUND = 512;                              // logits that may reach
 // (x = log2 e d)
 struct RowSums { float m, rest, xsum; };
 
-// ln p of a logit; log_s = log1p(rest).  In fp64: the difference of two fp32 numbers may be none.  (Code that a row passes once is kept short throughout: few rows find none of it in the
-// instruction cache, and 64 bytes of it cost 100 cycles then.)
+// ln p of a logit; log_s = log1p(rest).  In fp64: the difference of two fp32 numbers need not be one.  (Code that a row passes once
+// is kept short throughout: few rows find none of it in the instruction cache, and 64 bytes of it cost 100 cycles then.)
 __device__ __forceinline__ float log_p(const RowSums &r, float log_s, float z, float tau)
 {
     return r.rest == -1.f ? -__builtin_inff() : (float)(((double)z - (double)r.m) / (double)tau - (double)log_s);      // (-1: nothing but -inf)
@@ -468,22 +474,21 @@ template <int DT> __global__ __launch_bounds__(JOIN_THREADS) void head_join_kern
     const float log_s = log1pf(r.rest);
     if (tid == JOIN_THREADS - 64) finish_row(a, row, r, log_s, target, target_z);
     if (n > 0) {
-        constexpr int EACH = MAX_PARTS * MAX_N / JOIN_THREADS;
         __shared__ uint64_t found[MAX_PARTS * MAX_N];
         __shared__ uint32_t wave_bound[JOIN_WAVES];
         __shared__ int n_found;
-        uint64_t key[EACH], most = 0;
         // all parts' first keys, then their second, ...: a thread's first is its largest or close to it
-        int p = tid % parts, rank = tid / parts;
-        const int dp = JOIN_THREADS % parts, dr = JOIN_THREADS / parts;
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) {
-            key[i] = rank < n ? in.keys[(row * parts + p) * n + rank] : 0;
-            rank += dr + (p + dp >= parts);
-            p += p + dp >= parts ? dp - parts : dp;
-        }
-#pragma unroll
-        for (int i = 0; i < EACH; ++i) most = key[i] > most ? key[i] : most;
+        auto each_key = [&](auto take) __attribute__((always_inline)) {
+            const int dp = JOIN_THREADS % parts, dr = JOIN_THREADS / parts;
+#pragma unroll 1
+            for (int p = tid % parts, rank = tid / parts; rank < n;) {
+                take(in.keys[(row * parts + p) * n + rank]);
+                rank += dr + (p + dp >= parts);
+                p += p + dp >= parts ? dp - parts : dp;
+            }
+        };
+        uint64_t most = 0;
+        each_key([&](uint64_t key) __attribute__((always_inline)) { most = key > most ? key : most; });
         const uint32_t reached = bound_of((uint32_t)(most >> 32), (n + JOIN_WAVES - 1) / JOIN_WAVES);
         if (lane == 0) wave_bound[tid >> 6] = reached;
         if (tid == 0) n_found = 0;
@@ -491,9 +496,9 @@ template <int DT> __global__ __launch_bounds__(JOIN_THREADS) void head_join_kern
         uint32_t bound = wave_bound[0];
 #pragma unroll
         for (int w = 1; w < JOIN_WAVES; ++w) bound = min(bound, wave_bound[w]);
-#pragma unroll
-        for (int i = 0; i < EACH; ++i)
-            if (key[i] && (uint32_t)(key[i] >> 32) >= bound) found[atomicAdd(&n_found, 1)] = key[i];
+        each_key([&](uint64_t key) __attribute__((always_inline)) {
+            if (key && (uint32_t)(key >> 32) >= bound) found[atomicAdd(&n_found, 1)] = key;
+        });
         __syncthreads();
         ranked<JOIN_THREADS>(found, n_found, n, [&](int rank, uint64_t k) {
             a.top_idx[row * n + rank] = key_id(k);
@@ -513,27 +518,27 @@ int64_t longest_part(int threads, int per)
     return bits < owners ? (bits < MAX_PART ? bits : MAX_PART) : (owners < MAX_PART ? owners : MAX_PART);
 }
 
-// A row is one workgroup's unless there are few and long ones: a second launch costs what 64 K logits take (T rows, one part / four
-// of 38 K: 8 rows of 151,936 14.8 / 10.7 us, 64 15.8 / 11.4, 256 18.9 / 21.9, 8 of 32,000 6.8 / 10.9).
-constexpr int CUT_FROM = 65536, CUT_LEN = 32768, CUT_WORKGROUPS = 512;
-// A wavefront a row where rows are short and many (no barrier waits for another; 8192 rows of 2048: 64 / 256 threads 16 / 30 us; of
-// 8192 36 / 35, with 20 alternatives 51 / 57); not for more alternatives than half its lanes, whose bound is too low (1024 rows of 2048,
-// 64 alternatives: 102 / 14).  Two workgroups' threads for few long rows (256 of 151,936: 256 / 512 threads 21.1 / 18.9 us; 1024
-// 71 / 71; 64 of 32,000 6.6 / 7.3).
-constexpr int SHORT_ROW = 8192, MANY_ROWS = 1024, FEW_ROWS = 256;
+// A row is one workgroup's unless it is long and there are few of it, because a second launch costs what 64 K logits take (bf16, with
+// entropy, uncut / cut, us: 65,536 logits, 1 row 8.3 / 11.2; 102,400, 32 rows 12.5 / 10.9; 128 rows with 20 alternatives 16.9 / 20.7;
+// 151,936, 1 row 15.7 / 11.1; 64 rows 17.1 / 13.2; 128 rows 17.5 / 17.1, with alternatives 20.9 / 25.5; 262,144, 96 rows 25.1 / 18.1).
+constexpr int CUT_FROM = 98304, CUT_LEN = 32768, CUT_ROWS = 2048;
+// A wavefront a row where rows are short and many, since nothing waits at a barrier then (64 / 256 threads, us: 8192 rows of 2048
+// 16 / 30; of 8192 36 / 35, with 20 alternatives 51 / 57); not for more alternatives than half its lanes, whose bound would be too low
+// (1024 rows of 2048, 64 alternatives: 102 / 14).  Twice the threads for long rows as long as every compute unit has one at most
+// (256 / 512 threads: 256 rows of 151,936 21.1 / 18.9; 333 of 102,400 20.5 / 22.4; 64 of 32,000 6.6 / 7.3).
+constexpr int LONG_ROW = 65536, SHORT_ROW = 8192, MANY_ROWS = 1024, FEW_ROWS = 256;
 
-// entries: alternatives or a teacher's tokens
 Cut cut_rows(int dtype, int V, int64_t T, int top_n, int K)
 {
     const int per = dtype == REMOE_BF16 ? 8 : 4;
     int threads = 256;
-    if (V >= CUT_FROM && T <= FEW_ROWS) threads = 512;
+    if (V >= LONG_ROW && T <= FEW_ROWS) threads = 512;
     else if (V <= SHORT_ROW && T >= MANY_ROWS && top_n <= 32) threads = 64;
     while (threads > 64 && V < threads * per) threads >>= 1;  // every lane has a piece
     while (threads < K) threads <<= 1;                        // and a teacher's every entry a thread
     int64_t parts = ceil_div(V, longest_part(threads, per));
     const int64_t more = ceil_div(V, CUT_LEN);
-    if (V >= CUT_FROM && T * more <= CUT_WORKGROUPS && parts < more) parts = more < MAX_PARTS ? more : MAX_PARTS;
+    if (V >= CUT_FROM && T <= V / CUT_ROWS && parts < more) parts = more < MAX_PARTS ? more : MAX_PARTS;
     const int64_t len = align_up(ceil_div(V, parts), threads * per);
     return {threads, (int)ceil_div(V, len), (int)len};
 }
@@ -565,9 +570,8 @@ template <int NT> remoe_status launch_scan(const HeadArgs &a, const Cut &cut, co
 // (The parts of a row depend neither on the alternatives nor on the teacher's list, which only matter to shorter rows.)
 size_t head_workspace_bytes(int dtype, int V, int64_t T, int top_n)
 {
-    const int64_t more = ceil_div(V, CUT_LEN), most = CUT_WORKGROUPS / (more < CUT_WORKGROUPS ? more : CUT_WORKGROUPS);
-    const int64_t always = ceil_div(V, MAX_PART);
-    int64_t slots = V >= CUT_FROM ? (T < most ? T : most) * cut_rows(dtype, V, 1, 0, 0).parts : 0;
+    const int64_t few = V >= CUT_FROM ? V / CUT_ROWS : 0, always = ceil_div(V, MAX_PART);
+    int64_t slots = (T < few ? T : few) * cut_rows(dtype, V, 1, 0, 0).parts;
     if (always > 1 && slots < T * always) slots = T * always;
     return align_up(sizeof(RowSums) * (size_t)slots, 256) + align_up(sizeof(uint64_t) * (size_t)slots * top_n, 256) + 256;
 }

@@ -51,7 +51,9 @@ __global__ __launch_bounds__(NT) void head_grad_kernel(const HeadGradArgs a, int
     int head = (int)((16 - ((uintptr_t)dz & 15)) & 15) / (int)sizeof(elem);
     if (head > V) head = V;
     const int pieces = (V - head) / P::N;
-    const int p0 = seg * seg_pieces, p1 = seg == segs - 1 || p0 + seg_pieces > pieces ? pieces : p0 + seg_pieces;
+    // (the stretches are cut for a row whose first value is aligned: another one may have two pieces less)
+    const int p0 = seg * seg_pieces < pieces ? seg * seg_pieces : pieces;
+    const int p1 = seg == segs - 1 || p0 + seg_pieces > pieces ? pieces : p0 + seg_pieces;
     const int v0 = seg == 0 ? 0 : head + p0 * P::N, v1 = seg == segs - 1 ? V : head + p1 * P::N;      // this workgroup's values
 
     // the first pieces are on their way while the row's terms are put together

@@ -560,7 +560,7 @@ def test_long_rows_with_fewer_tokens_than_asked_for(T, V, n):
     _check_logprobs(_logprobs(_to_device(z), 1.0, tgt, n), z, 1.0, tgt, n)
 
 
-@pytest.mark.parametrize("T,V,dtype", [(200, 70001, BF16), (300, 70001, BF16), (100, 65536, F32), (102, 151936, BF16), (103, 151936, BF16)])
+@pytest.mark.parametrize("T,V,dtype", [(200, 70001, BF16), (300, 70001, BF16), (100, 65536, F32), (74, 151936, BF16), (75, 151936, BF16), (47, 98304, F32), (49, 98304, F32)])
 def test_where_rows_are_dealt_out_otherwise(T, V, dtype):
     print(f"threads and parts T={T} V={V} {dtype}", flush=True)
     z = rows(T, [("plain", "masked", "ties", "few")[t % 4] for t in range(T)], V, dtype)
@@ -600,3 +600,17 @@ def test_gradients_of_many_short_rows(V):
     for K, accumulate in ((1, False), (64, True), (65, False)):
         idx, tl, lse = _teacher(V + K, z, K)
         _distill_gradient(z, 1.0, idx, tl, lse if K == 64 else None, d, accumulate=accumulate)
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+def test_named_tokens_behind_the_last_piece(shift):
+    """2,093,057 values are 261,633 pieces in 512 stretches; shifted by one value they are 261,631, and the last stretch has none of
+    them, only the two values behind them."""
+    V = 8 * (511 * 512 + 1) - 7
+    z = rows(81, ("plain",), V, BF16)
+    one = torch.ones(1)
+    for t in (V - 1, V - 2, V - 3, 0, 6, 7):
+        print(f"target {t} shift {shift}", flush=True)
+        _logprob_gradient(z, 1.0, torch.tensor([t], dtype=torch.int32), one, None, shift_d=shift)
+    idx = torch.tensor([[V - 1, 5, V - 2]], dtype=torch.int32)
+    _distill_gradient(z, 1.0, idx, torch.tensor([[1.0, 2.0, 0.5]]), None, one, shift_d=shift)
