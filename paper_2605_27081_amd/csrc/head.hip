@@ -21,6 +21,8 @@
 // vector instructions (11.5 issue slots a bf16 logit, 4 of them the exponential) fill about nine tenths of the time; by those for less
 // than two rows a compute unit (333 rows of 102,400: 17 us); by latency for few (one row with 20 alternatives 9 + 6 us of kernels).  An
 // element at a time in three passes took 2530 us, 257 and 1767.
+#include <type_traits>
+
 #include "head_rows.h"
 #include "topk.h"
 
@@ -61,8 +63,8 @@ __device__ __forceinline__ float value_of(uint32_t order)
 __device__ __forceinline__ uint64_t rank_key(float z, int id) { return (uint64_t)order_of(z) << 32 | (0xFFFFFFFFu - (uint32_t)id); }
 __device__ __forceinline__ int key_id(uint64_t key) { return (int)(0xFFFFFFFFu - (uint32_t)key); }
 
-// x = log2 e d from a difference of logits.  log2 e / tau is not an fp32 number: what is cut off it would make every exponential
-// wrong in the same direction, by up to 2^-23 |d|, so it is multiplied in as well.
+// Exponents to base 2.  C = log2 e / tau is not an fp32 number: what is cut off it would make every exponential wrong in the same
+// direction, by up to 2^-23 |d|, so it is kept in two.
 struct Scale {
     float c, low;                                             // c rounded towards 0; low > 0, so that -inf stays -inf
     __device__ __forceinline__ explicit Scale(float tau)
@@ -71,14 +73,20 @@ struct Scale {
         c = __double2float_rz(all);
         low = fmaxf((float)(all - (double)c), 1e-30f);
     }
-    __device__ __forceinline__ float x(float d) const { return fmaf(d, low, d * c); }
+    // C d of a difference of logits
+    __device__ __forceinline__ float of_difference(float d) const { return fmaf(d, low, d * c); }
+    // C z - ref, each rounded as the result is: two instructions a logit where a difference first takes three
+    __device__ __forceinline__ float against(float z, float ref) const { return fmaf(z, low, fmaf(z, c, -ref)); }
+    // A reference for sums over logits up to z: C z, to 2^-24 of it.  Beyond 2^26 that would be off by more than a few, which an
+    // exponential does not forgive: there it stays at 2^26 and is of no use unless a larger logit takes over.
+    __device__ __forceinline__ float reference(float z) const { return __builtin_amdgcn_fmed3f(z * c, -0x1p26f, 0x1p26f); }
+    __device__ __forceinline__ bool refers(float z) const { return fabsf(z * c) < 0x1p26f; }
 };
 
-// The scale from sums relative to `from` to sums relative to `to`, and the shift of x.  2^-512 is 0, and the floor keeps
-// -inf out of products with 0.
+// From sums relative to 2^from to sums relative to 2^(from - shift): 2^-512 is 0, and the floor keeps -inf out of products with 0.
 struct Rescale {
     float dx, f;
-    __device__ __forceinline__ Rescale(float from, float to, const Scale &c) : dx(fmaxf(c.x(from - to), -512.f)), f(__builtin_amdgcn_exp2f(dx)) {}
+    __device__ __forceinline__ explicit Rescale(float shift) : dx(fmaxf(shift, -512.f)), f(__builtin_amdgcn_exp2f(dx)) {}
 };
 
 // The outputs of a row that one thread writes, from its sums.  target, target_z: its token and that one's logit.
@@ -230,7 +238,8 @@ struct PartOut {              // a part's results in the workspace
     uint64_t *keys;           // [T, parts, n], descending, 0 where there are fewer
 };
 
-template <int NT, int DT, bool ENTROPY, bool TOP, bool TEACHER>
+// ONCE: loads of the stream that leave nothing in the caches.
+template <int NT, int DT, bool ENTROPY, bool TOP, bool TEACHER, bool ONCE>
 __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int parts, int part_len, PartOut out)
 {
     typedef typename LogitOf<DT>::type elem;
@@ -258,15 +267,16 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
     const Scale c(a.tau);
 
     u32x4_t next[PIECES];
+    // (the last piece again where there is none: no branch, and no registers to be set beforehand)
     auto request = [&](int batch) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) {
             const int at = (batch * PIECES + u) * NT + tid;
-            next[u] = P::lowest();
-            if (at < pieces) next[u] = *reinterpret_cast<const u32x4_t *>(zp + (int64_t)at * P::N);
+            const auto *from = reinterpret_cast<const u32x4_t *>(reinterpret_cast<const char *>(zp) + (uint32_t)(at < pieces ? at : pieces - 1) * 16u);
+            next[u] = ONCE ? __builtin_nontemporal_load(from) : *from;
         }
     };
-    request(0);
+    if (batches > 0) request(0);
     int target = -1;
     float target_z = 0.f;
     if (parts == 1) request_target(a, row, z, target, target_z);
@@ -274,29 +284,39 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
     const int edge_at = tid < head ? tid : tid >= 32 && tid - 32 < len - behind ? behind + tid - 32 : -1;
     const float edge = edge_at >= 0 ? widen(zs[edge_at]) : -__builtin_inff();
 
-    // m: largest so far; s, xs: sums relative to ref, which is m, or the lowest number there is
-    float m = edge, ref = fmaxf(edge, LOWEST), s = 0.f, xs = 0.f;
-    if (edge_at >= 0) s = __builtin_amdgcn_exp2f(c.x(edge - ref));
+    // m: largest so far; s, xs: sum 2^x and sum x 2^x, x relative to ref, which follows m
+    float m = edge, ref = c.reference(fmaxf(edge, LOWEST)), s = 0.f, xs = 0.f;
+    if (edge_at >= 0) {
+        const float x = c.against(edge, ref);
+        s = __builtin_amdgcn_exp2f(x);
+        if constexpr (ENTROPY) xs = fmaxf(x, -512.f) * s;
+    }
     if constexpr (TOP) block_max[batches * NT + tid] = edge;
     for (int b = 0; b < batches; ++b) {
+        if (b + 1 == batches)
+#pragma unroll
+            for (int u = 0; u < PIECES; ++u)
+                if ((b * PIECES + u) * NT + tid >= pieces) next[u] = P::lowest();
         float v[BATCH];
 #pragma unroll
         for (int u = 0; u < PIECES; ++u) P::get(next[u], v + u * P::N);
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) asm volatile("" : "+v"(v[i]));        // taken out of `next` here, so that its registers are free
         if (b + 1 < batches) request(b + 1);
         float bm = v[0];
 #pragma unroll
         for (int i = 1; i < BATCH; ++i) bm = fmaxf(bm, v[i]);
         if constexpr (TOP) block_max[b * NT + tid] = bm;
         m = fmaxf(m, bm);
-        const float to = fmaxf(m, LOWEST);
-        const Rescale r(ref, to, c);
+        const float to = c.reference(fmaxf(m, LOWEST));
+        const Rescale r(ref - to);
         ref = to;
         if constexpr (ENTROPY) xs = r.f * (xs + r.dx * s);
         s *= r.f;
         float s4[4] = {0.f, 0.f, 0.f, 0.f}, x4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            const float x = c.x(v[i] - to), e = __builtin_amdgcn_exp2f(x);
+            const float x = c.against(v[i], to), e = __builtin_amdgcn_exp2f(x);
             s4[i & 3] += e;
             if constexpr (ENTROPY) x4[i & 3] = fmaf(fmaxf(x, -512.f), e, x4[i & 3]);
         }
@@ -327,7 +347,6 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
             top = wave_m[w];
             owner = w * 64 + wave_first[w];
         }
-    const float to = fmaxf(top, LOWEST);
     u32x4_t own = P::lowest();                                // a piece of the owner's
     if (tid * NT + owner < pieces) own = *reinterpret_cast<const u32x4_t *>(zp + (int64_t)(tid * NT + owner) * P::N);
     float least = 0.f;                                        // logits that reach it may be alternatives
@@ -352,22 +371,43 @@ __global__ __launch_bounds__(NT) void head_scan_kernel(const HeadArgs a, int par
             }
         }
     }
-    {
-        const Rescale r(ref, to, c);
+    // sums relative to 2^(C top)
+    if (c.refers(top)) {
+        const float to = c.reference(top);
+        const Rescale r((ref - to) - c.against(top, to));
         if constexpr (ENTROPY) xs = r.f * (xs + r.dx * s);
         s *= r.f;
+    } else if (top > -__builtin_inff()) {                     // from the differences then, in a pass of its own
+        s = xs = 0.f;
+        auto add = [&](float z) __attribute__((always_inline)) {
+            const float x = c.of_difference(z - top), e = __builtin_amdgcn_exp2f(x);
+            s += e;
+            if constexpr (ENTROPY) xs = fmaf(fmaxf(x, -512.f), e, xs);
+        };
+        if (edge_at >= 0) add(edge);
+#pragma unroll 1
+        for (int i = tid; i < pieces; i += NT) {
+            float v[P::N];
+            P::get(*reinterpret_cast<const u32x4_t *>(zp + (int64_t)i * P::N), v);
+#pragma unroll
+            for (int k = 0; k < P::N; ++k) add(v[k]);
+        }
     }
     // the owner's logits once more: those below the largest, and how many equal it
     float equal = 0.f, again = 0.f;
     {
-        if (tid == owner) s = s == s ? 0.f : s;
+        if (tid == owner) {
+            s = s == s ? 0.f : s;
+            xs = 0.f;
+        }
         float v[P::N + 1];
         P::get(own, v);
         v[P::N] = tid == owner ? edge : -__builtin_inff();
 #pragma unroll
         for (int k = 0; k <= P::N; ++k) {
-            const float e = __builtin_amdgcn_exp2f(c.x(v[k] - to));
-            again += v[k] < top ? e : 0.f;
+            const float x = fmaxf(c.of_difference(v[k] - top), -512.f), e = v[k] < top ? __builtin_amdgcn_exp2f(x) : 0.f;
+            again += e;
+            if constexpr (ENTROPY) xs = fmaf(x, e, xs);
             equal += v[k] == top ? 1.f : 0.f;
         }
     }
@@ -466,7 +506,7 @@ template <int DT> __global__ __launch_bounds__(JOIN_THREADS) void head_join_kern
     const float top = wave_max(r.m);
     const uint64_t has = __ballot(r.m == top);
     const int owner = has ? __ffsll((unsigned long long)has) - 1 : 0;
-    const Rescale scale(fmaxf(r.m, LOWEST), fmaxf(top, LOWEST), c);
+    const Rescale scale(c.of_difference(fmaxf(r.m, LOWEST) - fmaxf(top, LOWEST)));
     const float whole = 1.f + r.rest;
     r.xsum = wave_sum(scale.f * (r.xsum + scale.dx * whole));
     r.rest = wave_sum(lane == owner ? r.rest : whole * scale.f);
@@ -543,19 +583,24 @@ Cut cut_rows(int dtype, int V, int64_t T, int top_n, int K)
     return {threads, (int)ceil_div(V, len), (int)len};
 }
 
+constexpr int64_t ROWS_UNDER_WAY = 7 * 256, LAST_LEVEL = (int64_t)256 << 20;
+
 template <int NT> remoe_status launch_scan(const HeadArgs &a, const Cut &cut, const PartOut &out, hipStream_t stream)
 {
     const bool bf16 = a.dtype == REMOE_BF16, entropy = a.entropy != nullptr, top = a.top_n > 0;
-    auto kernel = [&]() {
-        if (bf16) {
-            if (a.teacher_idx) return head_scan_kernel<NT, REMOE_BF16, false, false, true>;
-            if (top) return entropy ? head_scan_kernel<NT, REMOE_BF16, true, true, false> : head_scan_kernel<NT, REMOE_BF16, false, true, false>;
-            return entropy ? head_scan_kernel<NT, REMOE_BF16, true, false, false> : head_scan_kernel<NT, REMOE_BF16, false, false, false>;
-        }
-        if (a.teacher_idx) return head_scan_kernel<NT, REMOE_F32, false, false, true>;
-        if (top) return entropy ? head_scan_kernel<NT, REMOE_F32, true, true, false> : head_scan_kernel<NT, REMOE_F32, false, true, false>;
-        return entropy ? head_scan_kernel<NT, REMOE_F32, true, false, false> : head_scan_kernel<NT, REMOE_F32, false, false, false>;
-    }();
+    // Loads that leave nothing in the caches, unless alternatives are looked up again and the rows under way at a time fit the last
+    // level (with and without, us: 8192 rows of 151,936 381 / 433; 20 alternatives: 2048 rows of 151,936 127 / 139, 8192 of 32,000 126 / 117).
+    const int64_t under_way = a.T < ROWS_UNDER_WAY ? a.T : ROWS_UNDER_WAY;
+    const bool once = under_way * a.V * (bf16 ? 2 : 4) > LAST_LEVEL;
+    auto pick = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (a.teacher_idx) return head_scan_kernel<NT, DT, false, false, true, true>;
+        if (!top) return entropy ? head_scan_kernel<NT, DT, true, false, false, true> : head_scan_kernel<NT, DT, false, false, false, true>;
+        if constexpr (NT >= 256)                              // (shorter rows always fit)
+            if (once) return entropy ? head_scan_kernel<NT, DT, true, true, false, true> : head_scan_kernel<NT, DT, false, true, false, true>;
+        return entropy ? head_scan_kernel<NT, DT, true, true, false, false> : head_scan_kernel<NT, DT, false, true, false, false>;
+    };
+    auto kernel = bf16 ? pick(std::integral_constant<int, REMOE_BF16>()) : pick(std::integral_constant<int, REMOE_F32>());
     const int64_t longest = cut.len < a.V ? cut.len : a.V;
     const size_t lds = top ? sizeof(float) * NT * (ceil_div(longest, NT * BATCH) + 1) : 0;
     if (a.T * cut.parts * NT > 0xFFFFFFFFll)

@@ -65,8 +65,8 @@ __global__ __launch_bounds__(NT) void head_grad_kernel(const HeadGradArgs a, int
         for (int u = 0; u < PIECES; ++u) {
             const int at = p + u * NT;
             if (at < p1) {
-                in[u] = *reinterpret_cast<const u32x4_any_t *>(zp + (int64_t)at * P::N);
-                if constexpr (ADD) old[u] = *reinterpret_cast<const u32x4_t *>(dp + (int64_t)at * P::N);
+                in[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any_t *>(zp + (int64_t)at * P::N));
+                if constexpr (ADD) old[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t *>(dp + (int64_t)at * P::N));
             }
         }
     };

@@ -614,3 +614,19 @@ def test_named_tokens_behind_the_last_piece(shift):
         _logprob_gradient(z, 1.0, torch.tensor([t], dtype=torch.int32), one, None, shift_d=shift)
     idx = torch.tensor([[V - 1, 5, V - 2]], dtype=torch.int32)
     _distill_gradient(z, 1.0, idx, torch.tensor([[1.0, 2.0, 0.5]]), None, one, shift_d=shift)
+
+
+@pytest.mark.parametrize("scale", [1.0, 1e3, 1e5, 3e7, 5e7, 1e12])
+def test_large_logits(scale):
+    """Logits as large as a mistake in training makes them, up to where 2^-24 of one is many units, and down there too."""
+    for V in (9, 3000, 20011):
+        for dtype in (F32, BF16):
+            z = rows(91, ("plain", "peaked", "masked", "lowest", "ties", "equal"), V, dtype).contiguous()
+            for sign in (1.0, -1.0):
+                shifted = (z.float() + sign * scale).to(dtype)
+                shifted = torch.where(torch.isinf(z) | (z == torch.finfo(dtype).min), z, shifted)
+                tgt = _targets(3, shifted)
+                _check_logprobs(_logprobs(_to_device(shifted), 1.0, tgt, 7 if V > 9 else 3), shifted, 1.0, tgt, 7 if V > 9 else 3)
+                spread = (z.float() * scale).clamp(-3e38, 3e38).to(dtype)
+                spread = torch.where(torch.isinf(z), z, spread)
+                _check_logprobs(_logprobs(_to_device(spread), 1.0, tgt, 0), spread, 1.0, tgt, 0)
