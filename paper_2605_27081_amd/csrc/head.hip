@@ -17,10 +17,10 @@
 //
 // Long rows that are few are cut into parts; head_join_kernel puts the parts together.
 //
-// Bound by HBM for many rows: 8192 rows of 151,936 bf16 logits with entropy 434 us = 5.7 TB/s (8192 of 65,536 fp32: 6.1), where the
-// vector instructions (11.5 issue slots a bf16 logit, 4 of them the exponential) fill about nine tenths of the time; by those for less
-// than two rows a compute unit (333 rows of 102,400: 17 us); by latency for few (one row with 20 alternatives 9 + 6 us of kernels).  An
-// element at a time in three passes took 2530 us, 257 and 1767.
+// Bound by HBM for many rows: 8192 rows of 151,936 bf16 logits with entropy 381 us = 6.5 TB/s (8192 of 65,536 fp32 318 us, 6.8), where
+// the vector instructions (9.7 issue slots a bf16 logit, two of them the exponential) fill nine tenths of the time; by those for less
+// than two rows a compute unit (333 rows of 102,400: 16 us); by latency for few (one row with 20 alternatives 9 + 6 us of kernels).  An
+// element at a time in three passes took 2530 us, 257 (333 rows) and 1767 (one).
 #include <type_traits>
 
 #include "head_rows.h"
@@ -559,13 +559,13 @@ int64_t longest_part(int threads, int per)
 }
 
 // A row is one workgroup's unless it is long and there are few of it, because a second launch costs what 64 K logits take (bf16, with
-// entropy, uncut / cut, us: 65,536 logits, 1 row 8.3 / 11.2; 102,400, 32 rows 12.5 / 10.9; 128 rows with 20 alternatives 16.9 / 20.7;
-// 151,936, 1 row 15.7 / 11.1; 64 rows 17.1 / 13.2; 128 rows 17.5 / 17.1, with alternatives 20.9 / 25.5; 262,144, 96 rows 25.1 / 18.1).
+// entropy, uncut / cut, us: 65,536 logits, 1 row 7.5 / 11.0; 102,400, 32 rows 11.7 / 9.3; 128 rows with 20 alternatives 15.9 / 20.6;
+// 151,936, 1 row 14.2 / 9.4; 64 rows 15.1 / 11.7; 128 rows 15.5 / 16.3, with alternatives 19.1 / 24.6; 262,144, 96 rows 21.8 / 16.4).
 constexpr int CUT_FROM = 98304, CUT_LEN = 32768, CUT_ROWS = 2048;
-// A wavefront a row where rows are short and many, since nothing waits at a barrier then (64 / 256 threads, us: 8192 rows of 2048
-// 16 / 30; of 8192 36 / 35, with 20 alternatives 51 / 57); not for more alternatives than half its lanes, whose bound would be too low
-// (1024 rows of 2048, 64 alternatives: 102 / 14).  Twice the threads for long rows as long as every compute unit has one at most
-// (256 / 512 threads: 256 rows of 151,936 21.1 / 18.9; 333 of 102,400 20.5 / 22.4; 64 of 32,000 6.6 / 7.3).
+// A wavefront a row where rows are short and many, since nothing waits at a barrier then (256 / 64 threads, us: 8192 rows of 2048
+// 32.5 / 14.8; of 8192 37.4 / 31.4, with 20 alternatives 53.8 / 44.2); not for more alternatives than half its lanes, whose bound would
+// be too low (1024 rows of 2048, 64 alternatives: 15.7 / 102).  Twice the threads for long rows as long as every compute unit has one
+// at most (256 / 512 threads: 256 rows of 151,936 19.3 / 17.4; 333 of 102,400 19.2 / 21.1; 64 of 32,000 6.9 / 7.7).
 constexpr int LONG_ROW = 65536, SHORT_ROW = 8192, MANY_ROWS = 1024, FEW_ROWS = 256;
 
 Cut cut_rows(int dtype, int V, int64_t T, int top_n, int K)
@@ -589,7 +589,7 @@ template <int NT> remoe_status launch_scan(const HeadArgs &a, const Cut &cut, co
 {
     const bool bf16 = a.dtype == REMOE_BF16, entropy = a.entropy != nullptr, top = a.top_n > 0;
     // Loads that leave nothing in the caches, unless alternatives are looked up again and the rows under way at a time fit the last
-    // level (with and without, us: 8192 rows of 151,936 381 / 433; 20 alternatives: 2048 rows of 151,936 127 / 139, 8192 of 32,000 126 / 117).
+    // level (with and without, us: 8192 rows of 151,936 394 / 433; 20 alternatives: 2048 rows of 151,936 121 / 137, 8192 of 32,000 126 / 118).
     const int64_t under_way = a.T < ROWS_UNDER_WAY ? a.T : ROWS_UNDER_WAY;
     const bool once = under_way * a.V * (bf16 ? 2 : 4) > LAST_LEVEL;
     auto pick = [&](auto dt) {

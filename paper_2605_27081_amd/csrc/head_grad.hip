@@ -6,11 +6,14 @@
 // A pass over the row writes the terms that every token has; the tokens that are named (the target, the teacher's) are taken
 // from their logits in fp64 and written over it: their differences cancel where the model agrees (1 - p_v, M p_v - q_v).
 // A workgroup has a stretch of a row's 16-byte pieces, cut where dlogits is aligned, and the named tokens among its values.  The
-// first pieces are asked for before the row's terms are known, the next ones before the present ones are used, and the stores
-// go past the caches (non-temporal: 4096 rows of 151,936 with a teacher's list 586 -> 545 us).
+// first pieces are asked for before the row's terms are known, the next ones before the present ones are used; loads and stores
+// go past the caches (4096 rows of 151,936 with a teacher's list: loads 518 -> 498 us, stores 590 -> 498).
 //
-// Bound by HBM: every logit is read and every gradient written once.  8192 rows of 151,936 bf16 logits 970 us = 5.1 TB/s (a plain
-// copy of 4 GiB 4.7), with a list of 128 for 4096 rows 508 us = 4.9 TB/s; 1021 rows of 50,257 36 us.
+// Bound by HBM: every logit is read and every gradient written once.  8192 rows of 151,936 bf16 logits 954 us = 5.2 TB/s (a plain
+// copy of 4 GiB 4.8), with a list of 128 for 4096 rows 493 us = 5.1 TB/s; 1021 rows of 50,257 37 us.  An element at a time by a workgroup
+// a row took 1853, 998 and 127 us.
+#include <type_traits>
+
 #include "head_rows.h"
 
 namespace remoe {
@@ -36,7 +39,8 @@ template <bool FINE> __device__ __forceinline__ float term(const RowTerms &t, fl
 __device__ __forceinline__ void put_one(float *p, float v) { *p = v; }
 __device__ __forceinline__ void put_one(bf16_t *p, float v) { *p = (bf16_t)(pack_bf16x2(v, 0.f) & 0xFFFFu); }
 
-template <int NT, int DT, bool TEACHER, bool ADD>
+// KEEP: stores that may stay in the caches
+template <int NT, int DT, bool TEACHER, bool ADD, bool KEEP>
 __global__ __launch_bounds__(NT) void head_grad_kernel(const HeadGradArgs a, int segs, int seg_pieces)
 {
     typedef typename LogitOf<DT>::type elem;
@@ -163,7 +167,9 @@ __global__ __launch_bounds__(NT) void head_grad_kernel(const HeadGradArgs a, int
             if constexpr (ADD) P::get(add[u], w);
 #pragma unroll
             for (int i = 0; i < P::N; ++i) v[i] = ADD ? term<FINE>(t, v[i]) + w[i] : term<FINE>(t, v[i]);
-            __builtin_nontemporal_store(P::put(v), reinterpret_cast<u32x4_t *>(dp + (int64_t)(p + u * NT) * P::N));
+            u32x4_t *to = reinterpret_cast<u32x4_t *>(dp + (int64_t)(p + u * NT) * P::N);
+            if constexpr (KEEP) *to = P::put(v);
+            else __builtin_nontemporal_store(P::put(v), to);
         }
     }
     __syncthreads();
@@ -174,17 +180,20 @@ __global__ __launch_bounds__(NT) void head_grad_kernel(const HeadGradArgs a, int
 
 namespace {
 
+// Named tokens are stored a second time, which takes the rest of their line back from memory if it has left the caches: with more
+// than one in 256 the stores stay there (past the caches / kept, us: 8192 rows of 2048, 64 listed tokens 26.7 / 22.7; of 8192
+// 73 / 65; 333 of 102,400 fp32 52.8 / 56.4; 4096 of 151,936, 128 listed 498 / 590).
+constexpr int KEEP_FROM = 256;
+
 template <int NT> remoe_status launch_grad(const HeadGradArgs &a, int64_t segs, int seg_pieces, hipStream_t stream)
 {
-    auto kernel = [&]() {
-        const bool bf16 = a.dtype == REMOE_BF16;
-        if (a.teacher_idx) {
-            if (a.accumulate) return bf16 ? head_grad_kernel<NT, REMOE_BF16, true, true> : head_grad_kernel<NT, REMOE_F32, true, true>;
-            return bf16 ? head_grad_kernel<NT, REMOE_BF16, true, false> : head_grad_kernel<NT, REMOE_F32, true, false>;
-        }
-        if (a.accumulate) return bf16 ? head_grad_kernel<NT, REMOE_BF16, false, true> : head_grad_kernel<NT, REMOE_F32, false, true>;
-        return bf16 ? head_grad_kernel<NT, REMOE_BF16, false, false> : head_grad_kernel<NT, REMOE_F32, false, false>;
-    }();
+    auto pick = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (!a.teacher_idx) return a.accumulate ? head_grad_kernel<NT, DT, false, true, false> : head_grad_kernel<NT, DT, false, false, false>;
+        if ((int64_t)a.K * KEEP_FROM > a.V) return a.accumulate ? head_grad_kernel<NT, DT, true, true, true> : head_grad_kernel<NT, DT, true, false, true>;
+        return a.accumulate ? head_grad_kernel<NT, DT, true, true, false> : head_grad_kernel<NT, DT, true, false, false>;
+    };
+    auto kernel = a.dtype == REMOE_BF16 ? pick(std::integral_constant<int, REMOE_BF16>()) : pick(std::integral_constant<int, REMOE_F32>());
     hipLaunchKernelGGL(kernel, dim3((unsigned)(a.T * segs)), dim3(NT), 0, stream, a, (int)segs, seg_pieces);
     return check_hip(hipGetLastError(), "head_grad_kernel launch");
 }
@@ -192,9 +201,9 @@ template <int NT> remoe_status launch_grad(const HeadGradArgs &a, int64_t segs, 
 }  // namespace
 
 // Workgroups of 256 threads, enough of them to even out the compute units, each with at least 2 pieces a thread, or 4 where a
-// teacher's list is taken first (1024 rows of 8192: 1 / 2 pieces 9.9 / 8.1 us; 1024 of 32,000, 64 listed tokens: 2 / 4 pieces
-// 37.9 / 31.7; 333 of 102,400 fp32: 4096 / 8192 workgroups 60 / 53).  A wavefront a row where many rows are short: its sums over the
-// list wait for no other (8192 rows of 2048, 64 listed tokens: 256 / 64 threads 38.6 / 26.1 us; of 8192 66.5 / 71.2).
+// teacher's list is taken first (1024 rows of 8192: 1 / 2 pieces 9.0 / 8.2 us; 1024 of 32,000, 64 listed tokens: 2 / 4 pieces
+// 39.9 / 31.5; 333 of 102,400 fp32: 4096 / 8192 workgroups 59.8 / 52.8).  A wavefront a row where many rows are short: its sums over
+// the list wait for no other (256 / 64 threads, 8192 rows of 2048 18.0 / 14.5 us, with 64 listed tokens 39.5 / 26.7; of 8192 46.7 / 52.5).
 constexpr int WORKGROUPS = 8192, SHORT_PIECES = 512, MANY_ROWS = 1024;
 
 remoe_status launch_head_backward(const HeadGradArgs &a, hipStream_t stream)
