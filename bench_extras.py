@@ -1,6 +1,7 @@
 """Timings of the entry points built beyond the MoE-layer hot path, at the sizes of the Qwen3-30B-A3B
 shaped prefill workload: 768 (sequence, layer) traces of 4096 steps for the cache simulator, 16
-sequences of 4096 steps for the router regularisers, 65,536 tokens for the gate gradient.
+sequences of 4096 steps for the router regularisers, 65,536 tokens for the gate gradient; and 8192 rows of
+151,936 logits for the calls over the vocabulary.
 
     python bench_extras.py [--repeat 10]
 
@@ -118,6 +119,30 @@ def main():
     flops = 2.0 * S * T * N * H
     line("remoe_gate_grad", ms, flops=flops, tflops=round(flops / ms / 1e9, 1), peak_tflops=round(2500.0 / 3, 1),
          frac=round(3 * flops / ms / 1e9 / 2500.0, 3), bound="mfma (bf16, three products per fp32-accurate one)")
+
+    T, V, n, k = 8192, 151936, 20, 64
+    desc = remoe.HeadDesc(V, remoe.REMOE_BF16, 1.0)
+    logits = torch.empty(T, V, dtype=torch.bfloat16, device=DEV)
+    for a in range(0, T, 512):
+        logits[a:a + 512] = 2.5 * torch.randn(512, V, generator=g, device=DEV)
+    tgt = torch.randint(0, V, (T,), generator=g, device=DEV).int()
+    tid = torch.randint(0, V, (T, k), generator=g, device=DEV).int()
+    tl = torch.randn(T, k, generator=g, device=DEV)
+    lp, ent, loss = (torch.empty(T, device=DEV) for _ in range(3))
+    stats, grad = torch.empty(T, 2, device=DEV), torch.empty_like(logits)
+    ti, tlp = torch.empty(T, n, dtype=torch.int32, device=DEV), torch.empty(T, n, device=DEV)
+    up = torch.full((T,), -1.0 / T, device=DEV)
+    hws = torch.empty(remoe.remoe_head_workspace_bytes(desc, T, n), dtype=torch.uint8, device=DEV)
+    read = logits.numel() * 2
+    for name, moved, fn in (
+            ("remoe_token_logprobs", read, lambda: remoe.remoe_token_logprobs(desc, logits, tgt, lp, ent, None, None, stats, hws)),
+            ("remoe_token_logprobs[top 20]", read, lambda: remoe.remoe_token_logprobs(desc, logits, tgt, lp, ent, ti, tlp, stats, hws)),
+            ("remoe_token_logprobs_backward", 2 * read,
+             lambda: remoe.remoe_token_logprobs_backward(desc, logits, stats, tgt, up, None, None, grad)),
+            ("remoe_distill_forward", read, lambda: remoe.remoe_distill_forward(desc, logits, tid, tl, None, loss, stats, hws)),
+            ("remoe_distill_backward", 2 * read, lambda: remoe.remoe_distill_backward(desc, logits, stats, tid, tl, None, up, grad))):
+        ms = timed(fn, args.repeat)
+        line(name, ms, rows=T, vocab=V, bytes=moved, gb_per_s=round(moved / ms / 1e6, 1), bound="HBM")
     return 0
 
 
