@@ -630,3 +630,36 @@ def test_large_logits(scale):
                 spread = (z.float() * scale).clamp(-3e38, 3e38).to(dtype)
                 spread = torch.where(torch.isinf(z), z, spread)
                 _check_logprobs(_logprobs(_to_device(spread), 1.0, tgt, 0), spread, 1.0, tgt, 0)
+
+
+def test_the_largest_vocabulary():
+    """One row of 2^24 logits: 64 parts."""
+    V, n = 1 << 24, 64
+    z = rows(101, ("plain",), V, BF16)
+    tgt = torch.tensor([V - 1], dtype=torch.int32)
+    _check_logprobs(_logprobs(_to_device(z), 1.0, tgt, n), z, 1.0, tgt, n)
+    idx, tl, _ = _teacher(7, z, 100)
+    _distill_gradient(z, 1.0, idx, tl, None, torch.ones(1))
+
+
+def test_the_most_rows():
+    """2^22 rows of three logits against torch in fp64."""
+    T, V = 1 << 22, 3
+    g = torch.Generator(device=DEV).manual_seed(3)
+    zd = (3.0 * torch.randn(T, V, generator=g, device=DEV)).bfloat16()
+    tgt = torch.randint(0, V, (T,), generator=g, device=DEV).int()
+    desc = _desc(V, BF16, 1.0)
+    lp, ent, st, ti, tl = _out(T), _out(T), _out(T, 2), _out(T, 2, dtype=torch.int32), _out(T, 2)
+    ws, _ = _workspace(desc, T, 2)
+    remoe.remoe_token_logprobs(desc, zd, tgt, lp, ent, ti, tl, st, ws)
+    up, dz = torch.full((T,), -1.0, device=DEV), torch.empty_like(zd)
+    remoe.remoe_token_logprobs_backward(desc, zd, st, tgt, up, None, None, dz)
+    want = torch.log_softmax(zd.double(), 1)
+    at = tgt.long()[:, None]
+    # a row's error is that of one exponential and one logarithm: 16 steps of a number of at most the logits' range
+    assert ((lp.double() - want.gather(1, at)[:, 0]).abs() <= 16 * STEP * (1.0 + zd.double().abs().amax(1))).all()
+    assert ((ent.double() - torch.special.entr(want.exp()).sum(1)).abs() <= 64 * STEP).all()
+    order = torch.sort(zd.float(), dim=1, descending=True, stable=True).indices[:, :2]
+    assert torch.equal(ti.long(), order)
+    grad = want.exp().scatter_add_(1, at, torch.full_like(at, -1, dtype=torch.float64))
+    assert ((dz.double() - grad).abs() <= HALF[BF16] * grad.abs() + 64 * STEP).all()
