@@ -348,55 +348,53 @@ def remoe_gate_grad(dlogits: torch.Tensor, x: torch.Tensor, dw: torch.Tensor, wo
 
 
 # The calls over the vocabulary take a few microseconds for few rows, so their arguments are marshalled with few look-ups: the
-# current device is asked for once, its stream's handle without a Stream object around it (2.7 us).
-def _dense(t: Optional[torch.Tensor], what: str, shape, dtype: torch.dtype, dev: int):
-    """Pointer of a contiguous tensor of this shape and type on the current device (NULL for None)."""
+# current device is asked for once, its stream's handle without a Stream object around it (2.7 us), tensors by their number of
+# elements.
+def _dense(t: Optional[torch.Tensor], what: str, count: int, dtype: torch.dtype, dev: int):
+    """Pointer of a contiguous tensor of so many elements of this type on the current device (NULL for None)."""
     if t is None:
         return None
-    if t.get_device() != dev:
-        raise _elsewhere(t, what, dev)
-    if t.shape != shape or t.dtype is not dtype:
-        raise RemoeError(f"{what} must be {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if not t.is_contiguous():
-        raise RemoeError("tensors must be contiguous")
+    if t.numel() != count or t.dtype is not dtype or t.get_device() != dev or not t.is_contiguous():
+        raise _wrong(t, what, f"{dtype}, {count} elements", dev)
     return t.data_ptr()
 
 
-def _elsewhere(t: torch.Tensor, what: str, dev: int) -> RemoeError:
-    if not t.is_cuda:
-        return RemoeError("the library takes device tensors")
-    return RemoeError(f"{what} is on {t.device}, the current device is cuda:{dev}")
-
-
 def _rows(t: torch.Tensor, what: str, desc: HeadDesc, dev: int):
-    """Pointer and row stride of a [T, vocab] matrix of the descriptor's type whose rows are dense."""
-    if t.get_device() != dev:
-        raise _elsewhere(t, what, dev)
+    """Rows, pointer and row stride of a [T, vocab] matrix of the descriptor's type whose rows are dense."""
     vocab = desc.vocab
-    if t.dim() != 2 or t.shape[1] != vocab or t.dtype is not desc.torch_dtype:
-        raise RemoeError(f"{what} must be {desc.torch_dtype} [T, {vocab}], got {t.dtype} {list(t.shape)}")
+    if t.dim() != 2 or t.dtype is not (torch.bfloat16 if desc.dtype else torch.float32) or t.get_device() != dev:
+        raise _wrong(t, what, f"{desc.torch_dtype} [T, {vocab}]", dev)
+    n, width = t.shape
     ld, step = t.stride()
+    if width != vocab:
+        raise _wrong(t, what, f"{desc.torch_dtype} [T, {vocab}]", dev)
     if step != 1 and vocab > 1:
         raise RemoeError(f"the values of a row of {what} must follow each other")
-    return t.data_ptr(), max(ld, vocab) if t.shape[0] < 2 else ld
+    return n, t.data_ptr(), ld if n > 1 else max(ld, vocab)
+
+
+def _wrong(t: torch.Tensor, what: str, wanted: str, dev: int) -> RemoeError:
+    if not t.is_cuda:
+        return RemoeError("the library takes device tensors")
+    if t.get_device() != dev:
+        return RemoeError(f"{what} is on {t.device}, the current device is cuda:{dev}")
+    return RemoeError(f"{what} must be contiguous {wanted}: got {t.dtype} {list(t.shape)}, strides {list(t.stride())}")
 
 
 def _device(t: torch.Tensor) -> int:
     if not t.is_cuda:
         raise RemoeError("the library takes device tensors")
-    return torch.cuda.current_device()
-
-
-def _raw_stream(dev: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(dev)
+    return torch._C._cuda_getDevice()
 
 
 def _scratch(t: torch.Tensor, dev: int):
-    if t.get_device() != dev:
-        raise _elsewhere(t, "workspace", dev)
-    if not t.is_contiguous():
-        raise RemoeError("tensors must be contiguous")
+    if t.get_device() != dev or not t.is_contiguous():
+        raise _wrong(t, "workspace", "bytes", dev)
     return t.data_ptr(), t.nbytes
+
+
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_F32, _I32 = torch.float32, torch.int32
 
 
 def remoe_head_workspace_bytes(desc: HeadDesc, n_tokens: int, top_n: int = 0) -> int:
@@ -411,16 +409,15 @@ def remoe_token_logprobs(desc: HeadDesc, logits: torch.Tensor, targets: Optional
                          out_top_logprob: Optional[torch.Tensor], out_stats: Optional[torch.Tensor], workspace: torch.Tensor) -> None:
     """logits [T, V] with dense rows; targets int32 [T]; out_logprob, out_entropy fp32 [T]; out_top_idx int32 [T, n] and
     out_top_logprob fp32 [T, n]; out_stats fp32 [T, 2] (max, rest of the sum).  Outputs may be None."""
-    T, dev = logits.shape[0], _device(logits)
-    top_n = 0 if out_top_idx is None else out_top_idx.shape[-1]
-    z, ld = _rows(logits, "logits", desc, dev)
+    dev = _device(logits)
+    T, z, ld = _rows(logits, "logits", desc, dev)
     ws, ws_bytes = _scratch(workspace, dev)
+    top_n = 0 if out_top_idx is None else out_top_idx.shape[-1]
     _check(load_library().remoe_token_logprobs(
-        ctypes.byref(desc), z, T, ld, _dense(targets, "targets", (T,), torch.int32, dev), top_n,
-        _dense(out_logprob, "out_logprob", (T,), torch.float32, dev), _dense(out_entropy, "out_entropy", (T,), torch.float32, dev),
-        _dense(out_top_idx, "out_top_idx", (T, top_n), torch.int32, dev),
-        _dense(out_top_logprob, "out_top_logprob", (T, top_n), torch.float32, dev),
-        _dense(out_stats, "out_stats", (T, 2), torch.float32, dev), ws, ws_bytes, _raw_stream(dev)))
+        ctypes.byref(desc), z, T, ld, _dense(targets, "targets", T, _I32, dev), top_n, _dense(out_logprob, "out_logprob", T, _F32, dev),
+        _dense(out_entropy, "out_entropy", T, _F32, dev), _dense(out_top_idx, "out_top_idx", T * top_n, _I32, dev),
+        _dense(out_top_logprob, "out_top_logprob", T * top_n, _F32, dev), _dense(out_stats, "out_stats", 2 * T, _F32, dev), ws, ws_bytes,
+        _raw_stream(dev)))
 
 
 def remoe_token_logprobs_backward(desc: HeadDesc, logits: torch.Tensor, stats: torch.Tensor, targets: Optional[torch.Tensor],
@@ -428,26 +425,25 @@ def remoe_token_logprobs_backward(desc: HeadDesc, logits: torch.Tensor, stats: t
                                   dlogits: torch.Tensor, accumulate: bool = False) -> None:
     """stats fp32 [T, 2] and entropy fp32 [T] from remoe_token_logprobs; d_logprob, d_entropy fp32 [T]; dlogits [T, V] (written,
     or added to when accumulate; may be logits itself when not)."""
-    T, dev = logits.shape[0], _device(logits)
-    z, ld = _rows(logits, "logits", desc, dev)
-    dz, ld_d = _rows(dlogits, "dlogits", desc, dev)
-    if dlogits.shape[0] != T:
-        raise RemoeError(f"dlogits has {dlogits.shape[0]} rows, logits {T}")
+    dev = _device(logits)
+    T, z, ld = _rows(logits, "logits", desc, dev)
+    rows, dz, ld_d = _rows(dlogits, "dlogits", desc, dev)
+    if rows != T:
+        raise RemoeError(f"dlogits has {rows} rows, logits {T}")
     _check(load_library().remoe_token_logprobs_backward(
-        ctypes.byref(desc), z, T, ld, _dense(stats, "stats", (T, 2), torch.float32, dev), _dense(targets, "targets", (T,), torch.int32, dev),
-        _dense(d_logprob, "d_logprob", (T,), torch.float32, dev), _dense(entropy, "entropy", (T,), torch.float32, dev),
-        _dense(d_entropy, "d_entropy", (T,), torch.float32, dev), int(bool(accumulate)), dz, ld_d, _raw_stream(dev)))
+        ctypes.byref(desc), z, T, ld, _dense(stats, "stats", 2 * T, _F32, dev), _dense(targets, "targets", T, _I32, dev),
+        _dense(d_logprob, "d_logprob", T, _F32, dev), _dense(entropy, "entropy", T, _F32, dev), _dense(d_entropy, "d_entropy", T, _F32, dev),
+        bool(accumulate), dz, ld_d, _raw_stream(dev)))
 
 
-def _teacher(T: int, teacher_idx: torch.Tensor, teacher_logits: torch.Tensor, teacher_lse: Optional[torch.Tensor], dev: int):
-    if teacher_idx.dim() != 2:
-        raise RemoeError(f"teacher_idx must be [T, K], got {list(teacher_idx.shape)}")
-    K = teacher_idx.shape[1]
-    if teacher_logits.dtype not in (torch.float32, torch.bfloat16):
-        raise RemoeError(f"teacher_logits must be float32 or bfloat16, got {teacher_logits.dtype}")
-    code = REMOE_BF16 if teacher_logits.dtype == torch.bfloat16 else REMOE_F32
-    return (_dense(teacher_idx, "teacher_idx", (T, K), torch.int32, dev), _dense(teacher_logits, "teacher_logits", (T, K), teacher_logits.dtype, dev),
-            code, _dense(teacher_lse, "teacher_lse", (T,), torch.float32, dev), K)
+def _teacher(T: int, idx: torch.Tensor, logits: torch.Tensor, lse: Optional[torch.Tensor], dev: int):
+    if idx.dim() != 2:
+        raise RemoeError(f"teacher_idx must be [T, K], got {list(idx.shape)}")
+    K, dtype = idx.shape[1], logits.dtype
+    if dtype is not _F32 and dtype is not torch.bfloat16:
+        raise RemoeError(f"teacher_logits must be float32 or bfloat16, got {dtype}")
+    return (_dense(idx, "teacher_idx", T * K, _I32, dev), _dense(logits, "teacher_logits", T * K, dtype, dev),
+            REMOE_F32 if dtype is _F32 else REMOE_BF16, _dense(lse, "teacher_lse", T, _F32, dev), K)
 
 
 def remoe_distill_forward(desc: HeadDesc, logits: torch.Tensor, teacher_idx: torch.Tensor, teacher_logits: torch.Tensor,
@@ -455,24 +451,23 @@ def remoe_distill_forward(desc: HeadDesc, logits: torch.Tensor, teacher_idx: tor
                           workspace: torch.Tensor) -> None:
     """teacher_idx int32 [T, K], teacher_logits fp32 or bf16 [T, K], teacher_lse fp32 [T] or None; out_loss fp32 [T]; out_stats
     fp32 [T, 2] or None."""
-    T, dev = logits.shape[0], _device(logits)
-    z, ld = _rows(logits, "logits", desc, dev)
+    dev = _device(logits)
+    T, z, ld = _rows(logits, "logits", desc, dev)
     ws, ws_bytes = _scratch(workspace, dev)
     _check(load_library().remoe_distill_forward(
-        ctypes.byref(desc), z, T, ld, *_teacher(T, teacher_idx, teacher_logits, teacher_lse, dev),
-        _dense(out_loss, "out_loss", (T,), torch.float32, dev), _dense(out_stats, "out_stats", (T, 2), torch.float32, dev), ws, ws_bytes, _raw_stream(dev)))
+        ctypes.byref(desc), z, T, ld, *_teacher(T, teacher_idx, teacher_logits, teacher_lse, dev), _dense(out_loss, "out_loss", T, _F32, dev),
+        _dense(out_stats, "out_stats", 2 * T, _F32, dev), ws, ws_bytes, _raw_stream(dev)))
 
 
 def remoe_distill_backward(desc: HeadDesc, logits: torch.Tensor, stats: torch.Tensor, teacher_idx: torch.Tensor,
                            teacher_logits: torch.Tensor, teacher_lse: Optional[torch.Tensor], d_loss: torch.Tensor,
                            dlogits: torch.Tensor, accumulate: bool = False) -> None:
     """stats fp32 [T, 2] from remoe_distill_forward; d_loss fp32 [T]; dlogits as for remoe_token_logprobs_backward."""
-    T, dev = logits.shape[0], _device(logits)
-    z, ld = _rows(logits, "logits", desc, dev)
-    dz, ld_d = _rows(dlogits, "dlogits", desc, dev)
-    if dlogits.shape[0] != T:
-        raise RemoeError(f"dlogits has {dlogits.shape[0]} rows, logits {T}")
+    dev = _device(logits)
+    T, z, ld = _rows(logits, "logits", desc, dev)
+    rows, dz, ld_d = _rows(dlogits, "dlogits", desc, dev)
+    if rows != T:
+        raise RemoeError(f"dlogits has {rows} rows, logits {T}")
     _check(load_library().remoe_distill_backward(
-        ctypes.byref(desc), z, T, ld, _dense(stats, "stats", (T, 2), torch.float32, dev),
-        *_teacher(T, teacher_idx, teacher_logits, teacher_lse, dev), _dense(d_loss, "d_loss", (T,), torch.float32, dev), int(bool(accumulate)),
-        dz, ld_d, _raw_stream(dev)))
+        ctypes.byref(desc), z, T, ld, _dense(stats, "stats", 2 * T, _F32, dev), *_teacher(T, teacher_idx, teacher_logits, teacher_lse, dev),
+        _dense(d_loss, "d_loss", T, _F32, dev), bool(accumulate), dz, ld_d, _raw_stream(dev)))
