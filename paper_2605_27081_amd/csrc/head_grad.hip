@@ -126,6 +126,7 @@ __global__ __launch_bounds__(NT) void head_grad_kernel(const HeadGradArgs a, int
         }
         t.k0 = k0 * inv_s;
     }
+    if (empty) t.k0 = 0.f;               // whatever the gradient of an infinite loss is
     // the named token's value, before the pass below may write over its logit
     float exact = 0.f;
     if (named >= 0) {

@@ -616,6 +616,25 @@ def test_named_tokens_behind_the_last_piece(shift):
     _distill_gradient(z, 1.0, idx, torch.tensor([[1.0, 2.0, 0.5]]), None, one, shift_d=shift)
 
 
+@pytest.mark.parametrize("what", [float("inf"), float("-inf"), float("nan")])
+def test_rows_of_nothing_pass_no_gradient(what):
+    """Their loss is infinite, and so may be what a program makes of it."""
+    T, V = 3, 1003
+    z = torch.full((T, V), -torch.inf, dtype=BF16, device=DEV)
+    stats, entropy = _stats_on_device(z, 1.0)
+    tgt, up = torch.tensor([0, V - 1, -1], dtype=torch.int32, device=DEV), torch.full((T,), what, device=DEV)
+    for accumulate in (False, True):
+        prior = torch.arange(T * V, device=DEV).view(T, V).bfloat16()
+        want = prior if accumulate else torch.zeros_like(prior)
+        out = prior.clone()
+        remoe.remoe_token_logprobs_backward(_desc(V, BF16, 1.0), z, stats, tgt, up, entropy, up, out, accumulate)
+        assert torch.equal(out, want)
+        out = prior.clone()
+        idx = torch.tensor([[5, V - 1]] * T, dtype=torch.int32, device=DEV)
+        remoe.remoe_distill_backward(_desc(V, BF16, 1.0), z, stats, idx, torch.ones(T, 2, device=DEV), None, up, out, accumulate)
+        assert torch.equal(out, want)
+
+
 @pytest.mark.parametrize("scale", [1.0, 1e3, 1e5, 3e7, 5e7, 1e12])
 def test_large_logits(scale):
     """Logits as large as a mistake in training makes them, up to where 2^-24 of one is many units, and down there too."""
@@ -663,3 +682,6 @@ def test_the_most_rows():
     assert torch.equal(ti.long(), order)
     grad = want.exp().scatter_add_(1, at, torch.full_like(at, -1, dtype=torch.float64))
     assert ((dz.double() - grad).abs() <= HALF[BF16] * grad.abs() + 64 * STEP).all()
+    grad = torch.softmax(zd.double(), 1)
+    grad.scatter_add_(1, at, torch.full((T, 1), -1.0, dtype=torch.float64, device=DEV))
+    assert ((dz.double() - grad).abs() <= grad.abs() * (2.0 ** -8 + 256 * STEP) + 1e-15).all()     # (1e-15: 1 - p in torch's fp64)
