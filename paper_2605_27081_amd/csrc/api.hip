@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "common.h"
+#include "head_plan.h"
 
 namespace remoe {
 

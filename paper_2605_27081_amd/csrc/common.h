@@ -7,6 +7,7 @@
 
 #include "remoe.h"
 #include "remoe_bench.h"
+#include "sizes.h"
 
 namespace remoe {
 
@@ -30,9 +31,6 @@ remoe_status check_hip(hipError_t e, const char *what);
 
 // Compute units of the current device (looked up once per device).
 remoe_status compute_units(int *out);
-
-static inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-static inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // ---- device helpers ------------------------------------------------------------------------
 __device__ __forceinline__ float bf16_to_f32(bf16_t v) { return __uint_as_float(((uint32_t)v) << 16); }
@@ -207,7 +205,6 @@ struct HeadArgs {
     float *stats;             // [T, 2] or NULL
     void *workspace;
 };
-size_t head_workspace_bytes(int dtype, int V, int64_t T, int top_n);
 remoe_status launch_head_forward(const HeadArgs &a, hipStream_t stream);
 
 struct HeadGradArgs {

@@ -23,6 +23,7 @@
 // element at a time in three passes took 2530 us, 257 (333 rows) and 1767 (one).
 #include <type_traits>
 
+#include "head_plan.h"
 #include "head_rows.h"
 #include "topk.h"
 
@@ -32,16 +33,9 @@ namespace {
 
 constexpr float LN2 = 0.693147180559945309417f;
 constexpr float LOWEST = -3.402823466e38f;
-constexpr int BATCH = 32;                               // logits of a thread that are taken together
-constexpr int MAX_BATCHES = 32;                         // of a thread: bits of a mask
-constexpr int64_t MAX_PART = 1 << 18;                   // logits of a part
-constexpr int MAX_PARTS = 64;                           // a lane each in the join
+constexpr int BATCH = HEAD_BATCH;
 constexpr int MAX_N = 64;
 constexpr int FOUND = 512;                              // logits that may reach the bound
-
-// what the logits of a row, or of a part of it, add up to: largest, sum of the e^d without one of the largest, sum of x 2^x
-// (x = log2 e d)
-struct RowSums { float m, rest, xsum; };
 
 // ln p of a logit; log_s = log1p(rest).  In fp64: the difference of two fp32 numbers need not be one.  (Code that a row passes once
 // is kept short throughout: few rows find none of it in the instruction cache, and 64 bytes of it cost 100 cycles then.)
@@ -514,7 +508,7 @@ template <int DT> __global__ __launch_bounds__(JOIN_THREADS) void head_join_kern
     const float log_s = log1pf(r.rest);
     if (tid == JOIN_THREADS - 64) finish_row(a, row, r, log_s, target, target_z);
     if (n > 0) {
-        __shared__ uint64_t found[MAX_PARTS * MAX_N];
+        __shared__ uint64_t found[HEAD_MAX_PARTS * MAX_N];
         __shared__ uint32_t wave_bound[JOIN_WAVES];
         __shared__ int n_found;
         // all parts' first keys, then their second, ...: a thread's first is its largest or close to it
@@ -548,44 +542,9 @@ template <int DT> __global__ __launch_bounds__(JOIN_THREADS) void head_join_kern
     if (a.teacher_idx) finish_teacher<JOIN_THREADS>(a, row, z, r, part);
 }
 
-// How rows are dealt out: threads of a workgroup, parts of a row, logits of a part.
-struct Cut { int threads, parts, len; };
-
-// a bit of a mask for every batch of a thread, a thread for every piece of the owner's, no more LDS than lets four share a compute unit
-int64_t longest_part(int threads, int per)
-{
-    const int64_t bits = (int64_t)threads * BATCH * MAX_BATCHES, owners = (int64_t)threads * threads * per;
-    return bits < owners ? (bits < MAX_PART ? bits : MAX_PART) : (owners < MAX_PART ? owners : MAX_PART);
-}
-
-// A row is one workgroup's unless it is long and there are few of it, because a second launch costs what 64 K logits take (bf16, with
-// entropy, uncut / cut, us: 65,536 logits, 1 row 7.5 / 11.0; 102,400, 32 rows 11.7 / 9.3; 128 rows with 20 alternatives 15.9 / 20.6;
-// 151,936, 1 row 14.2 / 9.4; 64 rows 15.1 / 11.7; 128 rows 15.5 / 16.3, with alternatives 19.1 / 24.6; 262,144, 96 rows 21.8 / 16.4).
-constexpr int CUT_FROM = 98304, CUT_LEN = 32768, CUT_ROWS = 2048;
-// A wavefront a row where rows are short and many, since nothing waits at a barrier then (256 / 64 threads, us: 8192 rows of 2048
-// 32.5 / 14.8; of 8192 37.4 / 31.4, with 20 alternatives 53.8 / 44.2); not for more alternatives than half its lanes, whose bound would
-// be too low (1024 rows of 2048, 64 alternatives: 15.7 / 102).  Twice the threads for long rows as long as every compute unit has one
-// at most (256 / 512 threads: 256 rows of 151,936 19.3 / 17.4; 333 of 102,400 19.2 / 21.1; 64 of 32,000 6.9 / 7.7).
-constexpr int LONG_ROW = 65536, SHORT_ROW = 8192, MANY_ROWS = 1024, FEW_ROWS = 256;
-
-Cut cut_rows(int dtype, int V, int64_t T, int top_n, int K)
-{
-    const int per = dtype == REMOE_BF16 ? 8 : 4;
-    int threads = 256;
-    if (V >= LONG_ROW && T <= FEW_ROWS) threads = 512;
-    else if (V <= SHORT_ROW && T >= MANY_ROWS && top_n <= 32) threads = 64;
-    while (threads > 64 && V < threads * per) threads >>= 1;  // every lane has a piece
-    while (threads < K) threads <<= 1;                        // and a teacher's every entry a thread
-    int64_t parts = ceil_div(V, longest_part(threads, per));
-    const int64_t more = ceil_div(V, CUT_LEN);
-    if (V >= CUT_FROM && T <= V / CUT_ROWS && parts < more) parts = more < MAX_PARTS ? more : MAX_PARTS;
-    const int64_t len = align_up(ceil_div(V, parts), threads * per);
-    return {threads, (int)ceil_div(V, len), (int)len};
-}
-
 constexpr int64_t ROWS_UNDER_WAY = 7 * 256, LAST_LEVEL = (int64_t)256 << 20;
 
-template <int NT> remoe_status launch_scan(const HeadArgs &a, const Cut &cut, const PartOut &out, hipStream_t stream)
+template <int NT> remoe_status launch_scan(const HeadArgs &a, const HeadCut &cut, const PartOut &out, hipStream_t stream)
 {
     const bool bf16 = a.dtype == REMOE_BF16, entropy = a.entropy != nullptr, top = a.top_n > 0;
     // Loads that leave nothing in the caches, unless alternatives are looked up again and the rows under way at a time fit the last
@@ -611,23 +570,13 @@ template <int NT> remoe_status launch_scan(const HeadArgs &a, const Cut &cut, co
 
 }  // namespace
 
-// Never less for more tokens: so many rows as are cut because they are few, or all of them where a row is longer than a part.
-// (The parts of a row depend neither on the alternatives nor on the teacher's list, which only matter to shorter rows.)
-size_t head_workspace_bytes(int dtype, int V, int64_t T, int top_n)
-{
-    const int64_t few = V >= CUT_FROM ? V / CUT_ROWS : 0, always = ceil_div(V, MAX_PART);
-    int64_t slots = (T < few ? T : few) * cut_rows(dtype, V, 1, 0, 0).parts;
-    if (always > 1 && slots < T * always) slots = T * always;
-    return align_up(sizeof(RowSums) * (size_t)slots, 256) + align_up(sizeof(uint64_t) * (size_t)slots * top_n, 256) + 256;
-}
-
 remoe_status launch_head_forward(const HeadArgs &a, hipStream_t stream)
 {
-    const Cut cut = cut_rows(a.dtype, a.V, a.T, a.top_n, a.K);
+    const HeadCut cut = head_cut(a.dtype, a.V, a.T, a.top_n, a.K);
     PartOut out{};
     if (cut.parts > 1) {
         out.sums = static_cast<RowSums *>(a.workspace);
-        out.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(a.workspace) + align_up(sizeof(RowSums) * (size_t)(a.T * cut.parts), 256));
+        out.keys = reinterpret_cast<uint64_t *>(static_cast<char *>(a.workspace) + head_keys_at(a.T * cut.parts));
     }
     const remoe_status st = cut.threads == 64    ? launch_scan<64>(a, cut, out, stream)
                             : cut.threads == 128 ? launch_scan<128>(a, cut, out, stream)
