@@ -437,10 +437,16 @@ remoe_status remoe_gate_grad(const float *dlogits, const void *x, int32_t x_dtyp
  *   logits   rows of vocab consecutive values of desc->dtype, `ld` >= vocab values from one row to the next
  *            (values between vocab and ld are neither read nor written); any alignment of a value
  *   Arithmetic is fp32 from the logits on (fp64 for the few values per row where differences cancel); sums have a
- *   fixed order, results repeat bit for bit.  -inf masks a token: probability 0, gradient 0.  A row of nothing but
- *   -inf has stats (-inf, -1), ln p = -inf for every token, entropy 0 and gradient 0.  A row that holds NaN or +inf
- *   has rest = NaN (its max is unspecified), and its log probabilities, entropy, losses and gradients are NaN.
- *   vocab 1..2^24, temperature 2^-20..2^20, ld up to 2^32, n_tokens 0..2^22 (0 launches nothing).
+ *   fixed order, results repeat bit for bit (a row at another address modulo 16 is summed in another order).
+ *   -inf masks a token: probability 0, gradient 0.  A masked token that is named all the same keeps what its formula has
+ *   besides the probability: ln p is -inf and the gradient d_logprob / tau where it is the target; as a teacher's entry with
+ *   q > 0 it makes the loss +inf and has the gradient -q d_loss / tau.
+ *   A row of nothing but -inf has stats (-inf, -1), ln p = -inf for every token, entropy 0 and gradient 0 throughout.
+ *   A row that holds NaN or +inf has rest = NaN (its max is unspecified), and its log probabilities, entropy, losses and
+ *   gradients are NaN (a target outside 0..V-1 has log probability 0 there too).
+ *   vocab 1..2^24, temperature 2^-20..2^20, ld up to 2^32, n_tokens 0..2^22 (0 launches nothing).  Rows of more than 2^18
+ *   logits are taken in parts: the forward calls refuse (REMOE_E_UNSUPPORTED) more parts than one launch can count, and
+ *   n_tokens * ceil(vocab / 2^18) < 2^24 never is.
  */
 typedef struct {
     int32_t vocab;         /* V                                                                      */
