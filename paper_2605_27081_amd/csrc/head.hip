@@ -542,13 +542,17 @@ template <int DT> __global__ __launch_bounds__(JOIN_THREADS) void head_join_kern
     if (a.teacher_idx) finish_teacher<JOIN_THREADS>(a, row, z, r, part);
 }
 
+// (seven workgroups a compute unit by the bf16 kernels' registers, five by the fp32 ones')
 constexpr int64_t ROWS_UNDER_WAY = 7 * 256, LAST_LEVEL = (int64_t)256 << 20;
 
 template <int NT> remoe_status launch_scan(const HeadArgs &a, const HeadCut &cut, const PartOut &out, hipStream_t stream)
 {
     const bool bf16 = a.dtype == REMOE_BF16, entropy = a.entropy != nullptr, top = a.top_n > 0;
     // Loads that leave nothing in the caches, unless alternatives are looked up again and the rows under way at a time fit the last
-    // level (with and without, us: 8192 rows of 151,936 394 / 433; 20 alternatives: 2048 rows of 151,936 121 / 137, 8192 of 32,000 126 / 118).
+    // level (with and without, us: 8192 rows of 151,936 391 / 427, of 65,536 fp32 322 / 361; 4096 of 151,936 with a teacher's list
+    // 201 / 226; 512 of 50,257 14.6 / 15.2; 256 of 32,000 7.3 / 6.5; 20 alternatives: 2048 of 151,936 114 / 130, 8192 of 32,000 117 / 115;
+    // 64: 2048 of 32,000 42.1 / 41.2).  A call alone, that is; logits that fit the last level and are taken to their gradient next gain
+    // from loads that stay, which a launch cannot know (both calls: 700 of 151,936 128 / 117, 2048 of 32,000 78 / 73, fp32 153 / 134).
     const int64_t under_way = a.T < ROWS_UNDER_WAY ? a.T : ROWS_UNDER_WAY;
     const bool once = under_way * a.V * (bf16 ? 2 : 4) > LAST_LEVEL;
     auto pick = [&](auto dt) {

@@ -7,11 +7,13 @@
 // from their logits in fp64 and written over it: their differences cancel where the model agrees (1 - p_v, M p_v - q_v).
 // A workgroup has a stretch of a row's 16-byte pieces, cut where dlogits is aligned, and the named tokens among its values.  The
 // first pieces are asked for before the row's terms are known, the next ones before the present ones are used; loads and stores
-// go past the caches (4096 rows of 151,936 with a teacher's list: loads 518 -> 498 us, stores 590 -> 498).
+// go past the caches (4096 rows of 151,936 with a teacher's list: loads 518 -> 498 us, stores 590 -> 498; loads 1-5 % from 512 rows of
+// 50,257 on; stores 1000 -> 957 for 8192 of 151,936, and within 8 % either way where a copy of the gradient follows that fits the last level).
 //
 // Bound by HBM: every logit is read and every gradient written once.  8192 rows of 151,936 bf16 logits 954 us = 5.2 TB/s (a plain
-// copy of 4 GiB 4.8), with a list of 128 for 4096 rows 493 us = 5.1 TB/s; 1021 rows of 50,257 37 us.  An element at a time by a workgroup
-// a row took 1853, 998 and 127 us.
+// copy of 4 GiB 4.8), with a list of 128 for 4096 rows 493 us = 5.1 TB/s; 1021 rows of 50,257 37 us.  Accumulated, which reads
+// the gradient too: 1414 us = 5.3 TB/s, with the list 700 us = 5.3 TB/s (4096 rows of 65,536 fp32 590 us, 5.5; written only 420, 5.1).
+// An element at a time by a workgroup a row took 1853, 998 and 127 us.
 #include <type_traits>
 
 #include "head_rows.h"
@@ -204,7 +206,9 @@ template <int NT> remoe_status launch_grad(const HeadGradArgs &a, int64_t segs, 
 // Workgroups of 256 threads, enough of them to even out the compute units, each with at least 2 pieces a thread, or 4 where a
 // teacher's list is taken first (1024 rows of 8192: 1 / 2 pieces 9.0 / 8.2 us; 1024 of 32,000, 64 listed tokens: 2 / 4 pieces
 // 39.9 / 31.5; 333 of 102,400 fp32: 4096 / 8192 workgroups 59.8 / 52.8).  A wavefront a row where many rows are short: its sums over
-// the list wait for no other (256 / 64 threads, 8192 rows of 2048 18.0 / 14.5 us, with 64 listed tokens 39.5 / 26.7; of 8192 46.7 / 52.5).
+// the list wait for no other (256 / 64 threads, 8192 rows of 2048 18.0 / 14.5 us, with 64 listed tokens 39.5 / 26.7; of 8192 46.7 / 52.5);
+// a list of more than 64 needs the threads, one an entry.  Every workgroup takes the whole list before it stores, which short rows do
+// not hide (8192 bf16 rows, none / 64 / 65 / 128 / 256 listed, us: of 2048 14.4 / 22.9 / 42.3 / 54 / 97; of 8192 47 / 66 / 66 / 75 / 106).
 constexpr int WORKGROUPS = 8192, SHORT_PIECES = 512, MANY_ROWS = 1024;
 
 remoe_status launch_head_backward(const HeadGradArgs &a, hipStream_t stream)
